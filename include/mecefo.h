@@ -356,6 +356,130 @@ mecefo_status_t mecefo_block_bwd_skip_ex(const mecefo_ffn_desc_t* desc, const vo
     void* dX, void* dgamma, void* dWg, void* dWu, void* dWd, int accumulate,
     void* ws, size_t ws_bytes, void* hip_stream);
 
+/* ---- 8-bit activation checkpoints (Sec. 3.3 keeps one tensor per layer; here in half the bytes of bf16).
+ * A row is cut into groups of 32 columns; a group holds 32 signed bytes q and one byte e and stands for the values
+ * q * 2^(e - 127).  Packing: e - 127 is the exponent of the group's largest magnitude less 6 (not below -126), q is
+ * x * 2^(127 - e) rounded to the nearest whole number, halves to even, at most 127.  So |x - q 2^(e-127)| is at most
+ * half a step 2^(e-127), 1/128 of the group's largest magnitude, for every x of a bf16 tensor (for fp32 up to a whole step where x is beyond 127.5 steps).
+ * A group that holds an infinity or a NaN is stored as e = 255 and q = 0 and stands for NaN in all its columns.
+ * Every value that a checkpoint stands for is a bf16 number: unpacking is exact in either dtype.
+ * q [rows x ld_q]: 16-byte aligned, ld_q a multiple of 16 and >= 32 ceil(cols / 32); the columns behind cols are written as
+ * zeros.  e [rows x ld_e]: ld_e >= ceil(cols / 32).  Both below 2 GiB.  No part may overlap the tensor. */
+typedef struct {
+  void* q;
+  void* e;
+  int64_t ld_q, ld_e;
+} mecefo_ckpt_t;
+
+/* X [rows x cols] (row stride ldx; MECEFO_BF16: 16-byte aligned, ldx a multiple of 8) to a checkpoint and back. */
+mecefo_status_t mecefo_checkpoint_pack(mecefo_dtype_t dtype, const void* X, int64_t rows, int cols, int64_t ldx,
+    const mecefo_ckpt_t* ckpt, void* hip_stream);
+mecefo_status_t mecefo_checkpoint_unpack(mecefo_dtype_t dtype, const mecefo_ckpt_t* ckpt, int64_t rows, int cols,
+    void* X, int64_t ldx, void* hip_stream);
+
+/* mecefo_block_bwd_skip_ex with its stored tensors as checkpoints: H [b x d], and G and Z [b x f] or both NULL.
+ * Results are those of mecefo_block_bwd_skip_ex on the unpacked tensors, bit for bit.
+ * Workspace: mecefo_block_ckpt_workspace_bytes. */
+mecefo_status_t mecefo_block_ckpt_workspace_bytes(const mecefo_ffn_desc_t* desc, int r_gate, int r_up, int r_down,
+    size_t* out_bytes);
+mecefo_status_t mecefo_block_bwd_skip_ckpt(const mecefo_ffn_desc_t* desc, const mecefo_ckpt_t* H,
+    const void* dOut, const void* gamma,
+    const void* Wg, const void* Wu, const void* Wd,
+    mecefo_proj_t Pg, mecefo_proj_t Pu, mecefo_proj_t Pd, mecefo_side_t side,
+    const mecefo_ckpt_t* G, const mecefo_ckpt_t* Z, int exact_wgrad_mask,
+    void* dX, void* dgamma, void* dWg, void* dWu, void* dWd, int accumulate,
+    void* ws, size_t ws_bytes, void* hip_stream);
+
+/* The neighbor-mode stack that keeps every layer's H as a checkpoint: H is a host array of n_layers descriptors.
+ * The forward's X_out is that of mecefo_stack_fwd_neighbor.  Both calls: mecefo_stack_ckpt_workspace_bytes. */
+mecefo_status_t mecefo_stack_ckpt_workspace_bytes(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn,
+    int r_gate, int r_up, int r_down, size_t* out_bytes);
+mecefo_status_t mecefo_stack_fwd_neighbor_ckpt(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn,
+    int n_layers, const mecefo_layer_weights_t* layers, const void* X0, const mecefo_ckpt_t* H, void* X_out,
+    void* ws, size_t ws_bytes, void* hip_stream);
+mecefo_status_t mecefo_stack_bwd_skip_ckpt(const mecefo_ffn_desc_t* desc, int n_layers,
+    const mecefo_layer_weights_t* layers, const mecefo_ckpt_t* H, const mecefo_layer_lowrank_t* lowrank,
+    mecefo_side_t side, const void* dOut_top, void* dX_bottom, int accumulate,
+    void* ws, size_t ws_bytes, void* hip_stream);
+
+/* ---- LM head: log-probabilities of given tokens, and their gradient.  X [b x d] (ld_act_d) is the last block's output;
+ *   U = RMSNorm(X) * gamma, or X itself where gamma is NULL;  z = logit_scale * U W^T [b x V], W [V x d] (ld_w);
+ *   lse_i = log sum_v exp(z_iv);  logp_i = z_i,labels[i] - lse_i.
+ * A label outside [0, vocab) marks a token that is not scored: its logp is 0 (its lse is that of its row) and it has no
+ * part in the gradient, as far as its row of X is finite.
+ * The logits are never stored by the forward.  dtype MECEFO_BF16: products accumulated in fp32, exponentials and their
+ * sums in fp32; with gamma, U is rounded to bf16.  d_model must be a multiple of 8, vocab may be any size.
+ * The backward forms the products again and stores dz_iv = logit_scale * dlogp_i * ([v = labels[i]] - exp(z_iv - lse_i)) in
+ * dtype (b * up8(vocab) elements of the workspace, which must stay below 2 GiB: split the token batch and accumulate);
+ *   dU = dz W;  dX = dU through the norm's backward, or dU;  dW = dz^T U and dgamma in grad_dtype, overwritten or added to. */
+typedef struct {
+  int64_t tokens;               /* b */
+  int32_t d_model, vocab;       /* d, V */
+  int64_t ld_act_d, ld_w;       /* row strides of X and dX [b x d], of W and dW [V x d] */
+  mecefo_dtype_t dtype;         /* X, gamma, W, dX */
+  mecefo_dtype_t grad_dtype;    /* dW, dgamma: MECEFO_F32, or equal to dtype */
+  float logit_scale;            /* 1 / temperature; any finite number */
+  float rms_eps;                /* used only with gamma */
+} mecefo_head_desc_t;
+
+/* Workspace of the forward (backward = 0) or of the backward (1). */
+mecefo_status_t mecefo_head_workspace_bytes(const mecefo_head_desc_t* desc, int backward, size_t* out_bytes);
+/* labels, logp, lse [b]; lse may be NULL where no backward follows. */
+mecefo_status_t mecefo_head_logprob_fwd(const mecefo_head_desc_t* desc, const void* X, const void* gamma, const void* W,
+    const int64_t* labels, float* logp, float* lse, void* ws, size_t ws_bytes, void* hip_stream);
+/* lse: as the forward wrote it.  dlogp [b]: the gradient of every token's logp (read for scored tokens only).
+ * dX must not overlap X; dgamma may be NULL.  accumulate applies to dW and dgamma. */
+mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const void* X, const void* gamma, const void* W,
+    const int64_t* labels, const float* lse, const float* dlogp, void* dX, void* dgamma, void* dW, int accumulate,
+    void* ws, size_t ws_bytes, void* hip_stream);
+
+/* ---- Losses over token log-probabilities, and the gradient of every one of them.  Tokens lie packed, sequence k at
+ * [offsets[k], offsets[k + 1]) of the token arrays (offsets: device memory, not decreasing, within [0, tokens]; a sequence may
+ * be empty; offsets that break this give undefined results, but nothing outside the arrays is touched).  mask [tokens]: a token
+ * with 0 is not counted, and what the arrays hold for it is not used; NULL counts all.  dlogp [tokens] is written
+ * as a whole: zero for what is not counted or belongs to no sequence.  Sums are taken in fp64, in an order that depends on
+ * the sizes only.  All values fp32, at most 2^20 sequences. */
+
+/* Preference loss over pairs; sequence 2i is the preferred answer of pair i, sequence 2i + 1 the other one.
+ *   r_k = beta * sum over the counted tokens of (logp - ref_logp), or beta times their mean (length_mean; 0 for none);
+ *   h_i = r_2i - r_2i+1 - margin;
+ *   loss = mean over the pairs of -(1 - label_smoothing) log sigmoid(h_i) - label_smoothing log sigmoid(-h_i), 0 without pairs.
+ * ref_logp [tokens] may be NULL (0).  loss [1]; margins [pairs] = h and rewards [2 pairs] = r, either may be NULL;
+ * dlogp = grad_scale * d loss / d logp. */
+typedef struct {
+  int64_t tokens;
+  int32_t pairs;
+  float beta, label_smoothing, margin;
+  int32_t length_mean;
+  float grad_scale;
+} mecefo_preference_desc_t;
+mecefo_status_t mecefo_preference_workspace_bytes(const mecefo_preference_desc_t* desc, size_t* out_bytes);
+mecefo_status_t mecefo_preference_loss(const mecefo_preference_desc_t* desc, const float* logp, const float* ref_logp,
+    const uint8_t* mask, const int64_t* offsets, float* loss, float* margins, float* rewards, float* dlogp,
+    void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Clipped policy loss with a KL term.  For a counted token t with advantage A:
+ *   rho = exp(logp - old_logp);  q = ref_logp - logp;  KL = exp(q) - q - 1;
+ *   l = -min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A) + kl_coef * KL.
+ * loss = sum of w l with w = 1 / counted tokens (MECEFO_MEAN_TOKENS), or 1 / (counted tokens of the sequence * sequences that
+ * have any) (MECEFO_MEAN_SEQUENCES); 0 where nothing is counted.  kl and clipped: the same means of KL and of whether the bound
+ * is what min() takes; loss, kl and clipped are [1], the last two may be NULL.  A token on a bound still has its gradient.
+ * advantage: [tokens] (advantage_per_token) or [sequences].  ref_logp may be NULL where kl_coef is 0. */
+typedef enum { MECEFO_MEAN_TOKENS = 0, MECEFO_MEAN_SEQUENCES = 1 } mecefo_loss_mean_t;
+typedef struct {
+  int64_t tokens;
+  int32_t sequences;
+  float clip_low, clip_high;    /* clip_low in [0, 1] */
+  float kl_coef;
+  mecefo_loss_mean_t mean;
+  int32_t advantage_per_token;
+  float grad_scale;             /* dlogp = grad_scale * d loss / d logp */
+} mecefo_policy_desc_t;
+mecefo_status_t mecefo_policy_workspace_bytes(const mecefo_policy_desc_t* desc, size_t* out_bytes);
+mecefo_status_t mecefo_policy_loss(const mecefo_policy_desc_t* desc, const float* logp, const float* old_logp,
+    const float* ref_logp, const float* advantage, const uint8_t* mask, const int64_t* offsets,
+    float* loss, float* kl, float* clipped, float* dlogp, void* ws, size_t ws_bytes, void* hip_stream);
+
 /* Measurement aid (not part of the hot path; the only calls that create HIP objects).
  * After mecefo_profile_enable(n) every kernel stage enqueued by the calls above is bracketed
  * by a pair of HIP events on the call's own stream, for at most n stage launches.

@@ -74,10 +74,31 @@ class RefreshPolicy(C.Structure):
 
 
 MODE_STANDARD, MODE_NEIGHBOR = 0, 1
+MEAN_TOKENS, MEAN_SEQUENCES = 0, 1
 
 
 class SkipOptions(C.Structure):
     _fields_ = [("G", C.c_void_p), ("Z", C.c_void_p), ("exact_wgrad_mask", C.c_int32)]
+
+
+class Ckpt(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("e", C.c_void_p), ("ld_q", C.c_int64), ("ld_e", C.c_int64)]
+
+
+class HeadDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("d_model", C.c_int32), ("vocab", C.c_int32), ("ld_act_d", C.c_int64),
+                ("ld_w", C.c_int64), ("dtype", C.c_int), ("grad_dtype", C.c_int), ("logit_scale", C.c_float),
+                ("rms_eps", C.c_float)]
+
+
+class PreferenceDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("pairs", C.c_int32), ("beta", C.c_float), ("label_smoothing", C.c_float),
+                ("margin", C.c_float), ("length_mean", C.c_int32), ("grad_scale", C.c_float)]
+
+
+class PolicyDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("sequences", C.c_int32), ("clip_low", C.c_float), ("clip_high", C.c_float),
+                ("kl_coef", C.c_float), ("mean", C.c_int), ("advantage_per_token", C.c_int32), ("grad_scale", C.c_float)]
 
 
 class MecefoError(RuntimeError):
@@ -149,7 +170,31 @@ def lib() -> C.CDLL:
     L.mecefo_init.restype = C.c_int
     L.mecefo_set_option.argtypes = [C.c_char_p, C.c_char_p]
     L.mecefo_set_option.restype = C.c_int
-    for f in ("mecefo_workspace_bytes", "mecefo_ffn_fwd_recompute", "mecefo_ffn_bwd_exact",
+    K, S = C.POINTER(Ckpt), C.POINTER(C.c_size_t)
+    L.mecefo_checkpoint_pack.argtypes = [C.c_int, _vp, C.c_int64, C.c_int, C.c_int64, K, _vp]
+    L.mecefo_checkpoint_unpack.argtypes = [C.c_int, K, C.c_int64, C.c_int, _vp, C.c_int64, _vp]
+    L.mecefo_block_ckpt_workspace_bytes.argtypes = [D, C.c_int, C.c_int, C.c_int, S]
+    L.mecefo_block_bwd_skip_ckpt.argtypes = ([D, K] + [_vp] * 5 + [Proj] * 3 + [C.c_int, K, K, C.c_int] + [_vp] * 5 +
+                                             [C.c_int, _vp, C.c_size_t, _vp])
+    L.mecefo_stack_ckpt_workspace_bytes.argtypes = [D, C.POINTER(AttnDesc), C.c_int, C.c_int, C.c_int, S]
+    L.mecefo_stack_fwd_neighbor_ckpt.argtypes = [D, C.POINTER(AttnDesc), C.c_int, C.POINTER(LayerWeights), _vp, K, _vp, _vp,
+                                                 C.c_size_t, _vp]
+    L.mecefo_stack_bwd_skip_ckpt.argtypes = [D, C.c_int, C.POINTER(LayerWeights), K, C.POINTER(LayerLowrank), C.c_int, _vp, _vp,
+                                             C.c_int, _vp, C.c_size_t, _vp]
+    HD = C.POINTER(HeadDesc)
+    L.mecefo_head_workspace_bytes.argtypes = [HD, C.c_int, S]
+    L.mecefo_head_logprob_fwd.argtypes = [HD] + [_vp] * 6 + [_vp, C.c_size_t, _vp]
+    L.mecefo_head_logprob_bwd.argtypes = [HD] + [_vp] * 9 + [C.c_int, _vp, C.c_size_t, _vp]
+    L.mecefo_preference_workspace_bytes.argtypes = [C.POINTER(PreferenceDesc), S]
+    L.mecefo_preference_loss.argtypes = [C.POINTER(PreferenceDesc)] + [_vp] * 8 + [_vp, C.c_size_t, _vp]
+    L.mecefo_policy_workspace_bytes.argtypes = [C.POINTER(PolicyDesc), S]
+    L.mecefo_policy_loss.argtypes = [C.POINTER(PolicyDesc)] + [_vp] * 10 + [_vp, C.c_size_t, _vp]
+    for f in ("mecefo_checkpoint_pack", "mecefo_checkpoint_unpack", "mecefo_block_ckpt_workspace_bytes",
+              "mecefo_block_bwd_skip_ckpt", "mecefo_stack_ckpt_workspace_bytes", "mecefo_stack_fwd_neighbor_ckpt",
+              "mecefo_stack_bwd_skip_ckpt", "mecefo_head_workspace_bytes", "mecefo_head_logprob_fwd",
+              "mecefo_head_logprob_bwd", "mecefo_preference_workspace_bytes", "mecefo_preference_loss",
+              "mecefo_policy_workspace_bytes", "mecefo_policy_loss",
+              "mecefo_workspace_bytes", "mecefo_ffn_fwd_recompute", "mecefo_ffn_bwd_exact",
               "mecefo_ffn_bwd_lowrank", "mecefo_block_bwd_skip", "mecefo_block_full_workspace_bytes",
               "mecefo_block_bwd_full", "mecefo_projection_workspace_bytes", "mecefo_projection_refresh",
               "mecefo_block_fwd_workspace_bytes", "mecefo_block_fwd", "mecefo_grad_average", "mecefo_adamw_step",
@@ -387,6 +432,126 @@ def mecefo_projection_refresh(dtype, W, m, n, ldw, left, V0, ldv, r, power_iters
     p, nb = _ws(ws)
     _check(lib().mecefo_projection_refresh(dtype, _ptr(W), m, n, ldw, int(left), _ptr(V0), ldv, r, power_iters,
                                            cond_steps, polish_steps, _ptr(P), ldp, p, nb, _stream(stream)))
+
+
+def ckpt(q, e) -> Ckpt:
+    """Checkpoint argument from q [rows x >= 32 * groups] (int8) and e [rows x >= groups] (uint8), groups = ceil(cols / 32).
+    The struct holds raw device pointers; it also keeps references to the tensors."""
+    k = Ckpt(q.data_ptr(), e.data_ptr(), int(q.stride(0)), int(e.stride(0)))
+    k._tensors = (q, e)
+    return k
+
+
+def _kref(k):
+    return None if k is None else C.byref(k)
+
+
+def mecefo_checkpoint_pack(dtype, X, rows, cols, ldx, ckpt, stream=None):
+    _check(lib().mecefo_checkpoint_pack(dtype, _ptr(X), rows, cols, ldx, _kref(ckpt), _stream(stream)))
+
+
+def mecefo_checkpoint_unpack(dtype, ckpt, rows, cols, X, ldx, stream=None):
+    _check(lib().mecefo_checkpoint_unpack(dtype, _kref(ckpt), rows, cols, _ptr(X), ldx, _stream(stream)))
+
+
+def mecefo_block_ckpt_workspace_bytes(desc, r_gate=0, r_up=0, r_down=0) -> int:
+    out = C.c_size_t(0)
+    _check(lib().mecefo_block_ckpt_workspace_bytes(C.byref(desc), r_gate, r_up, r_down, C.byref(out)))
+    return out.value
+
+
+def mecefo_block_bwd_skip_ckpt(desc, H, dOut, gamma, Wg, Wu, Wd, Pg, Pu, Pd, side, dX, dgamma, dWg, dWu, dWd, accumulate,
+                               ws, G=None, Z=None, exact_wgrad_mask=0, stream=None):
+    """H, G, Z: ckpt(...) arguments."""
+    p, n = _ws(ws)
+    null = Proj(None, 0, 0)
+    _check(lib().mecefo_block_bwd_skip_ckpt(C.byref(desc), _kref(H), _ptr(dOut), _ptr(gamma), _ptr(Wg), _ptr(Wu), _ptr(Wd),
+                                            Pg or null, Pu or null, Pd or null, int(side), _kref(G), _kref(Z),
+                                            exact_wgrad_mask, _ptr(dX), _ptr(dgamma), _ptr(dWg), _ptr(dWu), _ptr(dWd),
+                                            int(accumulate), p, n, _stream(stream)))
+
+
+def ckpt_array(ckpts):
+    """ckpts: list of ckpt(...), one per layer."""
+    arr = (Ckpt * len(ckpts))(*ckpts)
+    arr._ckpts = list(ckpts)
+    return arr
+
+
+def mecefo_stack_ckpt_workspace_bytes(desc, attn, r_gate=0, r_up=0, r_down=0) -> int:
+    out = C.c_size_t(0)
+    _check(lib().mecefo_stack_ckpt_workspace_bytes(C.byref(desc), C.byref(attn), r_gate, r_up, r_down, C.byref(out)))
+    return out.value
+
+
+def mecefo_stack_fwd_neighbor_ckpt(desc, attn, layers, X0, H, X_out, ws, stream=None):
+    """H: ckpt_array(...)."""
+    p, n = _ws(ws)
+    _check(lib().mecefo_stack_fwd_neighbor_ckpt(C.byref(desc), C.byref(attn), len(layers), layers, _ptr(X0), H, _ptr(X_out),
+                                                p, n, _stream(stream)))
+
+
+def mecefo_stack_bwd_skip_ckpt(desc, layers, H, lowrank, side, dOut_top, dX_bottom, accumulate, ws, stream=None):
+    p, n = _ws(ws)
+    _check(lib().mecefo_stack_bwd_skip_ckpt(C.byref(desc), len(layers), layers, H, lowrank, int(side), _ptr(dOut_top),
+                                            _ptr(dX_bottom), int(accumulate), p, n, _stream(stream)))
+
+
+def make_head_desc(tokens, d_model, vocab, dtype, grad_dtype=F32, ld_act_d=None, ld_w=None, logit_scale=1.0,
+                   rms_eps=1e-6) -> HeadDesc:
+    return HeadDesc(tokens, d_model, vocab, ld_act_d or d_model, ld_w or d_model, dtype, grad_dtype, logit_scale, rms_eps)
+
+
+def mecefo_head_workspace_bytes(desc: HeadDesc, backward) -> int:
+    out = C.c_size_t(0)
+    _check(lib().mecefo_head_workspace_bytes(C.byref(desc), int(bool(backward)), C.byref(out)))
+    return out.value
+
+
+def mecefo_head_logprob_fwd(desc, X, gamma, W, labels, logp, lse, ws, stream=None):
+    p, n = _ws(ws)
+    _check(lib().mecefo_head_logprob_fwd(C.byref(desc), _ptr(X), _ptr(gamma), _ptr(W), _ptr(labels), _ptr(logp), _ptr(lse),
+                                         p, n, _stream(stream)))
+
+
+def mecefo_head_logprob_bwd(desc, X, gamma, W, labels, lse, dlogp, dX, dgamma, dW, accumulate, ws, stream=None):
+    p, n = _ws(ws)
+    _check(lib().mecefo_head_logprob_bwd(C.byref(desc), _ptr(X), _ptr(gamma), _ptr(W), _ptr(labels), _ptr(lse), _ptr(dlogp),
+                                         _ptr(dX), _ptr(dgamma), _ptr(dW), int(accumulate), p, n, _stream(stream)))
+
+
+def make_preference_desc(tokens, pairs, beta=0.1, label_smoothing=0.0, margin=0.0, length_mean=False,
+                         grad_scale=1.0) -> PreferenceDesc:
+    return PreferenceDesc(tokens, pairs, beta, label_smoothing, margin, int(bool(length_mean)), grad_scale)
+
+
+def mecefo_preference_workspace_bytes(desc: PreferenceDesc) -> int:
+    out = C.c_size_t(0)
+    _check(lib().mecefo_preference_workspace_bytes(C.byref(desc), C.byref(out)))
+    return out.value
+
+
+def mecefo_preference_loss(desc, logp, ref_logp, mask, offsets, loss, margins, rewards, dlogp, ws, stream=None):
+    p, n = _ws(ws)
+    _check(lib().mecefo_preference_loss(C.byref(desc), _ptr(logp), _ptr(ref_logp), _ptr(mask), _ptr(offsets), _ptr(loss),
+                                        _ptr(margins), _ptr(rewards), _ptr(dlogp), p, n, _stream(stream)))
+
+
+def make_policy_desc(tokens, sequences, clip_low=0.2, clip_high=0.2, kl_coef=0.0, mean=MEAN_TOKENS, advantage_per_token=False,
+                     grad_scale=1.0) -> PolicyDesc:
+    return PolicyDesc(tokens, sequences, clip_low, clip_high, kl_coef, mean, int(bool(advantage_per_token)), grad_scale)
+
+
+def mecefo_policy_workspace_bytes(desc: PolicyDesc) -> int:
+    out = C.c_size_t(0)
+    _check(lib().mecefo_policy_workspace_bytes(C.byref(desc), C.byref(out)))
+    return out.value
+
+
+def mecefo_policy_loss(desc, logp, old_logp, ref_logp, advantage, mask, offsets, loss, kl, clipped, dlogp, ws, stream=None):
+    p, n = _ws(ws)
+    _check(lib().mecefo_policy_loss(C.byref(desc), _ptr(logp), _ptr(old_logp), _ptr(ref_logp), _ptr(advantage), _ptr(mask),
+                                    _ptr(offsets), _ptr(loss), _ptr(kl), _ptr(clipped), _ptr(dlogp), p, n, _stream(stream)))
 
 
 STAGES = ["norm_fwd", "dgrad_down", "recompute", "swiglu_bwd", "dgrad_gate_up", "project", "contract",

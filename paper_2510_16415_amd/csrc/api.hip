@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "../../include/mecefo.h"
+#include "checkpoint.hip.h"
 #include "gemm_bf16_launch.hip.h"
 #include "mecefo_internal.h"
 
@@ -284,12 +285,13 @@ Workspace layout(const Ctx& c, const int r[3], mecefo_side_t side, int force_spl
 
 struct Bufs { char* base; Workspace w; };
 
-mecefo_status_t carve(const Ctx& c, const int r[3], mecefo_side_t side, void* ws, size_t ws_bytes, Bufs* out) {
+// tail: bytes that the caller needs behind the layout.
+mecefo_status_t carve(const Ctx& c, const int r[3], mecefo_side_t side, void* ws, size_t ws_bytes, Bufs* out, size_t tail = 0) {
   Workspace w = layout(c, r, side, 0, true);
-  if (w.total > ws_bytes) w = layout(c, r, side, 0, false);
-  while (w.total > ws_bytes && w.splits > 1) w = layout(c, r, side, w.splits - 1, false);
-  if (w.total > ws_bytes)
-    return fail(MECEFO_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, w.total);
+  if (w.total + tail > ws_bytes) w = layout(c, r, side, 0, false);
+  while (w.total + tail > ws_bytes && w.splits > 1) w = layout(c, r, side, w.splits - 1, false);
+  if (w.total + tail > ws_bytes)
+    return fail(MECEFO_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, w.total + tail);
   if (!ws) return fail(MECEFO_ERR_INVALID_ARG, "workspace is NULL");
   out->base = (char*)up((int64_t)(uintptr_t)ws, 256);
   out->w = w;
@@ -363,7 +365,7 @@ bool norm_rides(const Ctx& c) { return c.b * c.dm * c.esz <= (int64_t)4 << 20; }
 // (DG = dG, DZ = dZ, AA = A).   Sec. 3.3 (Rcomp).
 mecefo_status_t recompute(const Ctx& c, const Bufs& bf, const void* U, int64_t ldu, const void* dY,
                                     int64_t lddy, const void* Wg, const void* Wu, const void* Wd,
-                                    const void* Gsaved, const void* Zsaved, hipStream_t s, const SideJob* norm = nullptr) {
+                                    const void* Gsaved, const void* Zsaved, int64_t ldgz, hipStream_t s, const SideJob* norm = nullptr) {
   const mecefo_ffn_desc_t& d = *c.d;
   char* base = bf.base;
   void* DG = base + bf.w.DG; void* DZ = base + bf.w.DZ; void* AA = base + bf.w.AA;
@@ -393,7 +395,7 @@ mecefo_status_t recompute(const Ctx& c, const Bufs& bf, const void* U, int64_t l
   if (norm && !down.side_done) TRY(norm_forward(c, *norm, s));
   if (Gsaved) {
     STAGE(MECEFO_STAGE_SWIGLU_BWD, s);
-    HIP_TRY(launch_swiglu_bwd(c.bf16, Gsaved, Zsaved, d.ld_act_f, DG, DZ, AA, c.ldf, c.b, c.ff, (int)c.ldf, s));
+    HIP_TRY(launch_swiglu_bwd(c.bf16, Gsaved, Zsaved, ldgz, DG, DZ, AA, c.ldf, c.b, c.ff, (int)c.ldf, s));
   } else {
     STAGE(MECEFO_STAGE_RECOMPUTE, s);
     rec.clk = g_prof.cur_clk;
@@ -713,6 +715,106 @@ mecefo_status_t check_lowrank_args(const Ctx& c, const mecefo_proj_t P[3], mecef
   return MECEFO_OK;
 }
 
+// ---- neighbor-mode backward ------------------------------------------------------------------
+struct KeptCkpts { const mecefo_ckpt_t *H, *G, *Z; };
+// Room behind the workspace of the backward for the unpacked H, G and Z.
+size_t kept_bytes(const Ctx& c) {
+  return (size_t)(up(c.b * c.dm * c.esz, 256) + 2 * up(c.b * c.ldf * c.esz, 256)) + 256;
+}
+
+// The neighbor-mode backward behind its entry points.  kept: the stored tensors as 8-bit checkpoints, which are unpacked
+// into the workspace (H, opt->G and opt->Z are then NULL), or NULL.
+mecefo_status_t block_bwd_skip(const mecefo_ffn_desc_t* desc, const void* H, const KeptCkpts* kept, const void* dOut,
+                               const void* gamma, const void* Wg, const void* Wu, const void* Wd,
+                               mecefo_proj_t Pg, mecefo_proj_t Pu, mecefo_proj_t Pd, mecefo_side_t side,
+                               const mecefo_skip_options_t* opt, void* dX, void* dgamma, void* dWg,
+                               void* dWu, void* dWd, int accumulate, void* ws, size_t ws_bytes,
+                               void* hip_stream) {
+  Ctx c;
+  TRY(check_desc(desc, &c));
+  const void* Gs = opt ? opt->G : nullptr;
+  const void* Zs = opt ? opt->Z : nullptr;
+  const int exact_mask = opt ? opt->exact_wgrad_mask : 0;
+  if (exact_mask & ~7) return fail(MECEFO_ERR_INVALID_ARG, "exact_wgrad_mask has bits beyond gate (1), up (2), down (4)");
+  if ((Gs == nullptr) != (Zs == nullptr)) return fail(MECEFO_ERR_INVALID_ARG, "G and Z must both be given or both be NULL");
+  TRY(check_ptr(c, Gs, "G", false)); TRY(check_ptr(c, Zs, "Z", false));
+  Ckpt kh = {}, kg = {}, kz = {};
+  if (kept) {
+    TRY((mecefo_status_t)check_ckpt(kept->H, c.b, c.dm, "H", &kh));
+    if ((kept->G == nullptr) != (kept->Z == nullptr)) return fail(MECEFO_ERR_INVALID_ARG, "G and Z must both be given or both be NULL");
+    if (kept->G) {
+      TRY((mecefo_status_t)check_ckpt(kept->G, c.b, c.ff, "G", &kg));
+      TRY((mecefo_status_t)check_ckpt(kept->Z, c.b, c.ff, "Z", &kz));
+    }
+  }
+  TRY(check_ptr(c, H, "H", c.b > 0 && !kept)); TRY(check_ptr(c, dOut, "dOut", c.b > 0)); TRY(check_ptr(c, gamma, "gamma", false));
+  TRY(check_ptr(c, Wg, "Wg")); TRY(check_ptr(c, Wu, "Wu")); TRY(check_ptr(c, Wd, "Wd"));
+  TRY(check_ptr(c, dX, "dX", c.b > 0));
+  if (!dWg || !dWu || !dWd) return fail(MECEFO_ERR_INVALID_ARG, "dWg, dWu, dWd are required");
+  if (c.bf16 && (((uintptr_t)dWg | (uintptr_t)dWu | (uintptr_t)dWd) % 16)) return fail(MECEFO_ERR_INVALID_ARG, "gradient buffers must be 16-byte aligned");
+  if (dgamma && !gamma) return fail(MECEFO_ERR_INVALID_ARG, "dgamma requested but gamma is NULL");
+  TRY(check_alias(dX, "dX", dOut, "dOut", act_span(c, desc->ld_act_d)));
+  if (!kept) TRY(check_alias(dX, "dX", H, "H", act_span(c, desc->ld_act_d)));
+  const mecefo_proj_t P[3] = {Pg, Pu, Pd};
+  TRY(check_lowrank_args(c, P, side, exact_mask));
+  const int r[3] = {(exact_mask & 1) ? 0 : Pg.r, (exact_mask & 2) ? 0 : Pu.r, (exact_mask & 4) ? 0 : Pd.r};
+  Bufs bf;
+  TRY(carve(c, r, side, ws, ws_bytes, &bf, kept ? kept_bytes(c) : 0));
+  hipStream_t s = (hipStream_t)hip_stream;
+  char* base = bf.base;
+  int64_t ldh = desc->ld_act_d, ldgz = desc->ld_act_f;
+  if (kept && c.b > 0) {
+    char* at = base + bf.w.total;      // the layout's slack of 256 bytes lies in front
+    auto unpacked = [&](const Ckpt& k, int cols, int64_t ld) -> const void* {
+      void* X = at;
+      at += up(c.b * ld * c.esz, 256);
+      return launch_ckpt_unpack(c.bf16, k, c.b, cols, X, ld, s) == hipSuccess ? X : nullptr;
+    };
+    STAGE(MECEFO_STAGE_NORM_FWD, s);
+    ldh = c.dm;
+    ldgz = c.ldf;
+    H = unpacked(kh, c.dm, ldh);
+    if (kept->G) { Gs = unpacked(kg, c.ff, ldgz); Zs = unpacked(kz, c.ff, ldgz); }
+    if (!H || (kept->G && (!Gs || !Zs))) return fail(MECEFO_ERR_LAUNCH, "unpacking a checkpoint: %s", hipGetErrorString(hipGetLastError()));
+  }
+  const void* U = H;
+  int64_t ldu = ldh;
+  const SideJob norm = norm_job(c, H, ldh, gamma, base + bf.w.U, (float*)(base + bf.w.rstd));
+  const bool rides = gamma && c.b > 0 && norm_rides(c);
+  if (gamma && c.b > 0) {  // recompute the norm output from the stored tensor
+    if (!rides) TRY(norm_forward(c, norm, s));
+    U = base + bf.w.U;
+    ldu = c.dm;
+  }
+  void* dUb = base + bf.w.dU;
+  const LowRank q = low_rank(c, bf, U, ldu, dOut, desc->ld_act_d, P, side, exact_mask);
+  TRY(recompute(c, bf, U, ldu, dOut, desc->ld_act_d, Wg, Wu, Wd, Gs, Zs, ldgz, s, rides ? &norm : nullptr));
+  // Eq. (2) reads dOut (the down projection's output gradient) and, without a norm, H itself: when dX
+  // is a buffer of its own the norm backward goes first, while dU is still in the caches; when dX overwrites dOut (or H)
+  // it has to wait for the contraction, which needs the partial buffer.  The expand launch carries the sum of the gain
+  // gradient.
+  const bool dx_first = dX != dOut && dX != H;
+  Parts parts;
+  auto norm_args = [&]() {
+    return norm_bwd_args(c, bf, bf.w, parts, H, ldh, gamma, dOut, desc->ld_act_d, dX, desc->ld_act_d, dgamma != nullptr);
+  };
+  const bool read_parts = gamma && c.b > 0 && norm_bwd_reads_parts(c, bf, norm_args());
+  TRY(dgrad_and_project(c, bf, q, Wg, Wu, dUb, c.dm, s, read_parts ? &parts : nullptr));
+  // Skip the MHA connection: the gradient handed to the previous layer is dH = dOut + normbwd(dU).
+  SideJob later = {};
+  auto norm_bwd = [&]() -> mecefo_status_t {
+    if (gamma) return norm_backward(c, norm_args(), dgamma, accumulate, s, &later);
+    STAGE(MECEFO_STAGE_NORM_BWD, s);
+    if (c.b > 0) HIP_TRY(launch_add(c.bf16, dOut, desc->ld_act_d, dUb, c.dm, dX, desc->ld_act_d, c.b, c.dm, s));
+    return MECEFO_OK;
+  };
+  if (dx_first) TRY(norm_bwd());
+  void* dW[3] = {dWg, dWu, dWd};
+  TRY(wgrad_contract(c, bf, q, dW, accumulate, s));
+  if (!dx_first) TRY(norm_bwd());
+  return wgrad_expand(c, q, dW, accumulate, s, &later);
+}
+
 }  // namespace
 
 // ---- scratch of the entry point that allocates nothing ------------------------------------
@@ -891,7 +993,7 @@ mecefo_status_t mecefo_ffn_bwd_exact(const mecefo_ffn_desc_t* desc, const void* 
   Bufs bf;
   TRY(carve(c, r0, MECEFO_SIDE_INPUT, ws, ws_bytes, &bf));
   hipStream_t s = (hipStream_t)hip_stream;
-  TRY(recompute(c, bf, U, desc->ld_act_d, dY, desc->ld_act_d, Wg, Wu, Wd, G, Z, s));
+  TRY(recompute(c, bf, U, desc->ld_act_d, dY, desc->ld_act_d, Wg, Wu, Wd, G, Z, desc->ld_act_f, s));
   TRY(dgrad(c, bf, Wg, Wu, dU, desc->ld_act_d, s));
   // exact Wgrad: dWg = dG^T U, dWu = dZ^T U [f x d]; dWd = dY^T A [d x f]; contraction over tokens
   STAGE(MECEFO_STAGE_WGRAD_EXACT, s);
@@ -926,7 +1028,7 @@ mecefo_status_t mecefo_ffn_bwd_lowrank(const mecefo_ffn_desc_t* desc, const void
   TRY(carve(c, r, side, ws, ws_bytes, &bf));
   hipStream_t s = (hipStream_t)hip_stream;
   const LowRank q = low_rank(c, bf, U, desc->ld_act_d, dY, desc->ld_act_d, P, side, 0);
-  TRY(recompute(c, bf, U, desc->ld_act_d, dY, desc->ld_act_d, Wg, Wu, Wd, nullptr, nullptr, s));
+  TRY(recompute(c, bf, U, desc->ld_act_d, dY, desc->ld_act_d, Wg, Wu, Wd, nullptr, nullptr, 0, s));
   TRY(dgrad_and_project(c, bf, q, Wg, Wu, dU, desc->ld_act_d, s));
   void* dW[3] = {dWg, dWu, dWd};
   TRY(wgrad_contract(c, bf, q, dW, accumulate, s));
@@ -939,65 +1041,29 @@ mecefo_status_t mecefo_block_bwd_skip_ex(const mecefo_ffn_desc_t* desc, const vo
                                          const mecefo_skip_options_t* opt, void* dX, void* dgamma, void* dWg,
                                          void* dWu, void* dWd, int accumulate, void* ws, size_t ws_bytes,
                                          void* hip_stream) {
+  return block_bwd_skip(desc, H, nullptr, dOut, gamma, Wg, Wu, Wd, Pg, Pu, Pd, side, opt, dX, dgamma, dWg, dWu, dWd, accumulate,
+                        ws, ws_bytes, hip_stream);
+}
+
+mecefo_status_t mecefo_block_ckpt_workspace_bytes(const mecefo_ffn_desc_t* desc, int r_gate, int r_up, int r_down,
+                                                  size_t* out_bytes) {
   Ctx c;
+  TRY(mecefo_workspace_bytes(desc, r_gate, r_up, r_down, out_bytes));
   TRY(check_desc(desc, &c));
-  const void* Gs = opt ? opt->G : nullptr;
-  const void* Zs = opt ? opt->Z : nullptr;
-  const int exact_mask = opt ? opt->exact_wgrad_mask : 0;
-  if (exact_mask & ~7) return fail(MECEFO_ERR_INVALID_ARG, "exact_wgrad_mask has bits beyond gate (1), up (2), down (4)");
-  if ((Gs == nullptr) != (Zs == nullptr)) return fail(MECEFO_ERR_INVALID_ARG, "G and Z must both be given or both be NULL");
-  TRY(check_ptr(c, Gs, "G", false)); TRY(check_ptr(c, Zs, "Z", false));
-  TRY(check_ptr(c, H, "H", c.b > 0)); TRY(check_ptr(c, dOut, "dOut", c.b > 0)); TRY(check_ptr(c, gamma, "gamma", false));
-  TRY(check_ptr(c, Wg, "Wg")); TRY(check_ptr(c, Wu, "Wu")); TRY(check_ptr(c, Wd, "Wd"));
-  TRY(check_ptr(c, dX, "dX", c.b > 0));
-  if (!dWg || !dWu || !dWd) return fail(MECEFO_ERR_INVALID_ARG, "dWg, dWu, dWd are required");
-  if (c.bf16 && (((uintptr_t)dWg | (uintptr_t)dWu | (uintptr_t)dWd) % 16)) return fail(MECEFO_ERR_INVALID_ARG, "gradient buffers must be 16-byte aligned");
-  if (dgamma && !gamma) return fail(MECEFO_ERR_INVALID_ARG, "dgamma requested but gamma is NULL");
-  TRY(check_alias(dX, "dX", dOut, "dOut", act_span(c, desc->ld_act_d)));
-  TRY(check_alias(dX, "dX", H, "H", act_span(c, desc->ld_act_d)));
-  const mecefo_proj_t P[3] = {Pg, Pu, Pd};
-  TRY(check_lowrank_args(c, P, side, exact_mask));
-  const int r[3] = {(exact_mask & 1) ? 0 : Pg.r, (exact_mask & 2) ? 0 : Pu.r, (exact_mask & 4) ? 0 : Pd.r};
-  Bufs bf;
-  TRY(carve(c, r, side, ws, ws_bytes, &bf));
-  hipStream_t s = (hipStream_t)hip_stream;
-  char* base = bf.base;
-  const void* U = H;
-  int64_t ldu = desc->ld_act_d;
-  const SideJob norm = norm_job(c, H, desc->ld_act_d, gamma, base + bf.w.U, (float*)(base + bf.w.rstd));
-  const bool rides = gamma && c.b > 0 && norm_rides(c);
-  if (gamma && c.b > 0) {  // recompute the norm output from the stored tensor
-    if (!rides) TRY(norm_forward(c, norm, s));
-    U = base + bf.w.U;
-    ldu = c.dm;
-  }
-  void* dUb = base + bf.w.dU;
-  const LowRank q = low_rank(c, bf, U, ldu, dOut, desc->ld_act_d, P, side, exact_mask);
-  TRY(recompute(c, bf, U, ldu, dOut, desc->ld_act_d, Wg, Wu, Wd, Gs, Zs, s, rides ? &norm : nullptr));
-  // Eq. (2) reads dOut (the down projection's output gradient) and, without a norm, H itself: when dX
-  // is a buffer of its own the norm backward goes first, while dU is still in the caches; when dX overwrites dOut (or H)
-  // it has to wait for the contraction, which needs the partial buffer.  The expand launch carries the sum of the gain
-  // gradient.
-  const bool dx_first = dX != dOut && dX != H;
-  Parts parts;
-  auto norm_args = [&]() {
-    return norm_bwd_args(c, bf, bf.w, parts, H, desc->ld_act_d, gamma, dOut, desc->ld_act_d, dX, desc->ld_act_d, dgamma != nullptr);
-  };
-  const bool read_parts = gamma && c.b > 0 && norm_bwd_reads_parts(c, bf, norm_args());
-  TRY(dgrad_and_project(c, bf, q, Wg, Wu, dUb, c.dm, s, read_parts ? &parts : nullptr));
-  // Skip the MHA connection: the gradient handed to the previous layer is dH = dOut + normbwd(dU).
-  SideJob later = {};
-  auto norm_bwd = [&]() -> mecefo_status_t {
-    if (gamma) return norm_backward(c, norm_args(), dgamma, accumulate, s, &later);
-    STAGE(MECEFO_STAGE_NORM_BWD, s);
-    if (c.b > 0) HIP_TRY(launch_add(c.bf16, dOut, desc->ld_act_d, dUb, c.dm, dX, desc->ld_act_d, c.b, c.dm, s));
-    return MECEFO_OK;
-  };
-  if (dx_first) TRY(norm_bwd());
-  void* dW[3] = {dWg, dWu, dWd};
-  TRY(wgrad_contract(c, bf, q, dW, accumulate, s));
-  if (!dx_first) TRY(norm_bwd());
-  return wgrad_expand(c, q, dW, accumulate, s, &later);
+  *out_bytes += kept_bytes(c);
+  return MECEFO_OK;
+}
+
+mecefo_status_t mecefo_block_bwd_skip_ckpt(const mecefo_ffn_desc_t* desc, const mecefo_ckpt_t* H, const void* dOut,
+                                           const void* gamma, const void* Wg, const void* Wu, const void* Wd,
+                                           mecefo_proj_t Pg, mecefo_proj_t Pu, mecefo_proj_t Pd, mecefo_side_t side,
+                                           const mecefo_ckpt_t* G, const mecefo_ckpt_t* Z, int exact_wgrad_mask, void* dX,
+                                           void* dgamma, void* dWg, void* dWu, void* dWd, int accumulate, void* ws,
+                                           size_t ws_bytes, void* hip_stream) {
+  const KeptCkpts kept = {H, G, Z};
+  const mecefo_skip_options_t opt = {nullptr, nullptr, exact_wgrad_mask};
+  return block_bwd_skip(desc, nullptr, &kept, dOut, gamma, Wg, Wu, Wd, Pg, Pu, Pd, side, &opt, dX, dgamma, dWg, dWu, dWd,
+                        accumulate, ws, ws_bytes, hip_stream);
 }
 
 mecefo_status_t mecefo_block_bwd_skip(const mecefo_ffn_desc_t* desc, const void* H, const void* dOut,
@@ -1070,7 +1136,7 @@ mecefo_status_t mecefo_block_bwd_full(const mecefo_ffn_desc_t* desc, const mecef
   const SideJob norm = norm_job(c, in->H, d.ld_act_d, in->g_ffn, Ub, rstd);
   const bool rides = any && norm_rides(c);
   if (any && !rides) TRY(norm_forward(c, norm, s));
-  TRY(recompute(c, bf, Ub, dm, in->dOut, d.ld_act_d, in->Wg, in->Wu, in->Wd, nullptr, nullptr, s, rides ? &norm : nullptr));
+  TRY(recompute(c, bf, Ub, dm, in->dOut, d.ld_act_d, in->Wg, in->Wu, in->Wd, nullptr, nullptr, 0, s, rides ? &norm : nullptr));
   Parts parts;
   auto ffn_norm = [&]() {
     return norm_bwd_args(c, bf, fw, parts, in->H, d.ld_act_d, in->g_ffn, in->dOut, d.ld_act_d, dH, dm, true);
@@ -1356,6 +1422,53 @@ mecefo_status_t block_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_
   }
   return MECEFO_OK;
 }
+
+// ---- stacks ---------------------------------------------------------------------------------
+mecefo_status_t check_ckpts(const Ctx& c, const mecefo_ckpt_t* kept, int n_layers) {
+  Ckpt k;
+  for (int l = 0; l < n_layers; ++l) TRY((mecefo_status_t)check_ckpt(&kept[l], c.b, c.dm, "H", &k));
+  return MECEFO_OK;
+}
+
+// The forward behind its two entry points: every layer's H stays as it is, or is kept as an 8-bit checkpoint.
+mecefo_status_t stack_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn, int n_layers,
+                          const mecefo_layer_weights_t* layers, const void* X0, void* const* H, const mecefo_ckpt_t* kept,
+                          void* X_out, void* ws, size_t ws_bytes, void* hip_stream) {
+  Ctx c;
+  TRY(check_desc(desc, &c));
+  TRY(check_attn(c, attn));
+  if (n_layers < 1) return fail(MECEFO_ERR_INVALID_ARG, "n_layers must be >= 1");
+  if (!layers || (!H && !kept)) return fail(MECEFO_ERR_INVALID_ARG, "layers and H are required");
+  if (kept) TRY(check_ckpts(c, kept, n_layers));
+  if (c.b > 0 && X_out == X0) return fail(MECEFO_ERR_INVALID_ARG, "X_out must not alias X0");
+  const FwdWs plan = fwd_layout(c, *attn);
+  const size_t inner = plan.total;
+  const size_t act = (size_t)up(c.b * desc->ld_act_d * c.esz, 256);
+  if (!ws) return fail(MECEFO_ERR_INVALID_ARG, "workspace is NULL");
+  char* base = (char*)up((int64_t)(uintptr_t)ws, 256);
+  const size_t lead = (size_t)(base - (char*)ws);
+  const size_t front = lead + (kept ? 3 : 2) * act;
+  if (front + inner > ws_bytes) return fail(MECEFO_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, front + inner);
+  void* pp[2] = {base, base + act};
+  void* inner_ws = (char*)ws + front;
+  const void* x = X0;
+  for (int l = 0; l < n_layers; ++l) {
+    const mecefo_layer_weights_t& w = layers[l];
+    mecefo_block_fwd_inputs_t in = {x, w.g_attn, w.g_ffn, w.Wq, w.Wk, w.Wv, w.Wo, w.Wg, w.Wu, w.Wd};
+    void* y = l == n_layers - 1 ? X_out : pp[l & 1];
+    mecefo_block_fwd_outputs_t out = {y, kept ? base + 2 * act : H[l], nullptr, nullptr, nullptr, nullptr, nullptr};
+    // every layer of the call uses the same workspace and layout: the angle tables of the first one serve them all
+    mecefo_status_t st = block_fwd(desc, attn, &in, &out, &plan, inner_ws, ws_bytes - front, hip_stream, l > 0);
+    if (st != MECEFO_OK) return st;
+    if (kept && c.b > 0) {
+      Ckpt k;
+      TRY((mecefo_status_t)check_ckpt(&kept[l], c.b, c.dm, "H", &k));
+      HIP_TRY(launch_ckpt_pack(c.bf16, out.H, desc->ld_act_d, c.b, c.dm, k, (hipStream_t)hip_stream));
+    }
+    x = y;
+  }
+  return MECEFO_OK;
+}
 }  // namespace
 
 extern "C" {
@@ -1376,33 +1489,7 @@ mecefo_status_t mecefo_stack_fwd_neighbor(const mecefo_ffn_desc_t* desc, const m
                                           int n_layers, const mecefo_layer_weights_t* layers, const void* X0,
                                           void* const* H, void* X_out, void* ws, size_t ws_bytes,
                                           void* hip_stream) {
-  Ctx c;
-  TRY(check_desc(desc, &c));
-  TRY(check_attn(c, attn));
-  if (n_layers < 1) return fail(MECEFO_ERR_INVALID_ARG, "n_layers must be >= 1");
-  if (!layers || !H) return fail(MECEFO_ERR_INVALID_ARG, "layers and H are required");
-  if (c.b > 0 && X_out == X0) return fail(MECEFO_ERR_INVALID_ARG, "X_out must not alias X0");
-  const FwdWs plan = fwd_layout(c, *attn);
-  const size_t inner = plan.total;
-  const size_t act = (size_t)up(c.b * desc->ld_act_d * c.esz, 256);
-  if (!ws) return fail(MECEFO_ERR_INVALID_ARG, "workspace is NULL");
-  char* base = (char*)up((int64_t)(uintptr_t)ws, 256);
-  const size_t lead = (size_t)(base - (char*)ws);
-  if (lead + 2 * act + inner > ws_bytes) return fail(MECEFO_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, lead + 2 * act + inner);
-  void* pp[2] = {base, base + act};
-  void* inner_ws = base + 2 * act;
-  const void* x = X0;
-  for (int l = 0; l < n_layers; ++l) {
-    const mecefo_layer_weights_t& w = layers[l];
-    mecefo_block_fwd_inputs_t in = {x, w.g_attn, w.g_ffn, w.Wq, w.Wk, w.Wv, w.Wo, w.Wg, w.Wu, w.Wd};
-    void* y = l == n_layers - 1 ? X_out : pp[l & 1];
-    mecefo_block_fwd_outputs_t out = {y, H[l], nullptr, nullptr, nullptr, nullptr, nullptr};
-    // every layer of the call uses the same workspace and layout: the angle tables of the first one serve them all
-    mecefo_status_t st = block_fwd(desc, attn, &in, &out, &plan, inner_ws, ws_bytes - lead - 2 * act, hip_stream, l > 0);
-    if (st != MECEFO_OK) return st;
-    x = y;
-  }
-  return MECEFO_OK;
+  return stack_fwd(desc, attn, n_layers, layers, X0, H, nullptr, X_out, ws, ws_bytes, hip_stream);
 }
 
 mecefo_status_t mecefo_stack_bwd_skip(const mecefo_ffn_desc_t* desc, int n_layers, const mecefo_layer_weights_t* layers,
@@ -1425,6 +1512,45 @@ mecefo_status_t mecefo_stack_bwd_skip(const mecefo_ffn_desc_t* desc, int n_layer
   return MECEFO_OK;
 }
 
+mecefo_status_t mecefo_stack_ckpt_workspace_bytes(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn,
+                                                  int r_gate, int r_up, int r_down, size_t* out_bytes) {
+  size_t fwd = 0, bwd = 0;
+  TRY(mecefo_block_fwd_workspace_bytes(desc, attn, &fwd));
+  TRY(mecefo_block_ckpt_workspace_bytes(desc, r_gate, r_up, r_down, &bwd));
+  if (!out_bytes) return fail(MECEFO_ERR_INVALID_ARG, "out_bytes is NULL");
+  // the forward has two activations for its ping-pong and one H in front of a block's workspace
+  const size_t act = (size_t)up((int64_t)desc->tokens * desc->ld_act_d * (desc->dtype == MECEFO_BF16 ? 2 : 4), 256);
+  fwd += 3 * act + 512;
+  *out_bytes = fwd > bwd ? fwd : bwd;
+  return MECEFO_OK;
+}
+
+mecefo_status_t mecefo_stack_fwd_neighbor_ckpt(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn, int n_layers,
+                                               const mecefo_layer_weights_t* layers, const void* X0, const mecefo_ckpt_t* H,
+                                               void* X_out, void* ws, size_t ws_bytes, void* hip_stream) {
+  if (!H) return fail(MECEFO_ERR_INVALID_ARG, "layers and H are required");
+  return stack_fwd(desc, attn, n_layers, layers, X0, nullptr, H, X_out, ws, ws_bytes, hip_stream);
+}
+
+mecefo_status_t mecefo_stack_bwd_skip_ckpt(const mecefo_ffn_desc_t* desc, int n_layers, const mecefo_layer_weights_t* layers,
+                                           const mecefo_ckpt_t* H, const mecefo_layer_lowrank_t* lowrank, mecefo_side_t side,
+                                           const void* dOut_top, void* dX_bottom, int accumulate, void* ws, size_t ws_bytes,
+                                           void* hip_stream) {
+  if (n_layers < 1) return fail(MECEFO_ERR_INVALID_ARG, "n_layers must be >= 1");
+  if (!layers || !H || !lowrank) return fail(MECEFO_ERR_INVALID_ARG, "layers, H and lowrank are required");
+  Ctx c;
+  TRY(check_desc(desc, &c));
+  TRY(check_ckpts(c, H, n_layers));
+  const void* g = dOut_top;
+  for (int l = n_layers - 1; l >= 0; --l) {
+    const mecefo_layer_weights_t& w = layers[l];
+    const mecefo_layer_lowrank_t& q = lowrank[l];
+    TRY(mecefo_block_bwd_skip_ckpt(desc, &H[l], g, w.g_ffn, w.Wg, w.Wu, w.Wd, q.Pg, q.Pu, q.Pd, side, nullptr, nullptr, 0,
+                                   dX_bottom, q.dg_ffn, q.dWg, q.dWu, q.dWd, accumulate, ws, ws_bytes, hip_stream));
+    g = dX_bottom;
+  }
+  return MECEFO_OK;
+}
 
 mecefo_status_t mecefo_block_bwd_skip_noalloc(const mecefo_ffn_desc_t* desc, const void* H, const void* dOut,
                                               const void* gamma, const void* Wg, const void* Wu, const void* Wd,

@@ -1,0 +1,307 @@
+// Log-probabilities of given tokens under the LM head, and their gradient: what lies between the last block's output and the
+// gradient that the stack takes back.
+//   U = norm(X) gamma (or X),  z = logit_scale U W^T [b x V],  lse_i = log sum_v exp z_iv,  logp_i = z_i,label - lse_i
+//   dz_iv = logit_scale dlogp_i (1[v = label_i] - exp(z_iv - lse_i)),  dU = dz W,  dW = dz^T U
+// Everything that is large is a product on the GEMM core: 2 b d V operations forward, 6 b d V backward (z is formed again).
+#include <math.h>
+#include <string.h>
+
+#include "../../include/mecefo.h"
+#include "gemm_bf16_launch.hip.h"
+#include "mecefo_internal.h"
+
+namespace mecefo {
+namespace {
+
+__device__ inline bool counted(int64_t label, int vocab) { return label >= 0 && label < vocab; }
+
+// lse and logp of a row of fp32 products z (before logit_scale), a workgroup per row.
+__global__ __launch_bounds__(256) void head_rows_kernel(const float* __restrict__ Z, int64_t ldz, int vocab, float scale,
+                                                        const int64_t* __restrict__ labels, float* __restrict__ logp,
+                                                        float* __restrict__ lse) {
+  __shared__ float red[4];
+  const int64_t row = blockIdx.x;
+  const float* z = Z + row * ldz;
+  float m = -INFINITY;
+  for (int v = threadIdx.x; v < vocab; v += 256) m = fmaxf(m, z[v] * scale);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  __syncthreads();
+  float s = 0.f;
+  for (int v = threadIdx.x; v < vocab; v += 256) s += expf(z[v] * scale - m);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  const float l = m + logf((red[0] + red[1]) + (red[2] + red[3]));
+  const int64_t label = labels[row];
+  logp[row] = counted(label, vocab) ? z[label] * scale - l : 0.f;
+  if (lse) lse[row] = l;
+}
+
+// dz of a row from its products, zeros behind the vocabulary.
+template <typename T>
+__global__ __launch_bounds__(256) void head_dz_kernel(const float* __restrict__ Z, int64_t ldz, int vocab, float scale,
+                                                      const int64_t* __restrict__ labels, const float* __restrict__ lse,
+                                                      const float* __restrict__ dlogp, T* __restrict__ dZ) {
+  const int64_t row = blockIdx.x;
+  const int64_t label = labels[row];
+  const float c = counted(label, vocab) ? dlogp[row] * scale : 0.f, l = lse[row];
+  const float* z = Z + row * ldz;
+  T* o = dZ + row * ldz;
+  for (int v = threadIdx.x; v < (int)ldz; v += 256)
+    o[v] = (T)(v < vocab && c != 0.f ? c * ((v == (int)label ? 1.f : 0.f) - expf(z[v] * scale - l)) : 0.f);
+}
+
+// out[row, 0 .. cols) = sum of the parts [k][row, col], in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void head_sum_kernel(const float* __restrict__ part, int parts, int64_t rows, int cols,
+                                                       T* __restrict__ out, int64_t ldo) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * cols) return;
+  const int64_t row = i / cols;
+  float s = part[i];
+  for (int k = 1; k < parts; ++k) s += part[(int64_t)k * rows * cols + i];
+  out[row * ldo + (i - row * cols)] = (T)s;
+}
+
+__global__ __launch_bounds__(256) void head_zero_kernel(uint32_t* p, int n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) p[i] = 0;
+}
+
+inline int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+
+struct Head {
+  const mecefo_head_desc_t* d;
+  bool bf16;
+  int esz, b, dm, vocab;
+  int64_t ldz;
+};
+
+#define FAIL(st, ...) ((mecefo_status_t)fail((int)(st), __VA_ARGS__))
+#define TRY(x) do { mecefo_status_t st__ = (x); if (st__ != MECEFO_OK) return st__; } while (0)
+#define HIP_TRY(x) do { hipError_t e__ = (x); if (e__ != hipSuccess) return FAIL(MECEFO_ERR_LAUNCH, "%s: %s", #x, hipGetErrorString(e__)); } while (0)
+
+mecefo_status_t check_desc(const mecefo_head_desc_t* d, Head* h) {
+  if (!d) return FAIL(MECEFO_ERR_INVALID_ARG, "descriptor is NULL");
+  if (d->dtype != MECEFO_F32 && d->dtype != MECEFO_BF16) return FAIL(MECEFO_ERR_INVALID_ARG, "dtype must be MECEFO_F32 or MECEFO_BF16");
+  if (d->grad_dtype != MECEFO_F32 && d->grad_dtype != d->dtype) return FAIL(MECEFO_ERR_UNSUPPORTED, "grad_dtype must be MECEFO_F32 or equal to dtype");
+  if (d->tokens < 0 || d->d_model < 1 || d->vocab < 1) return FAIL(MECEFO_ERR_INVALID_ARG, "tokens >= 0, d_model >= 1, vocab >= 1 required");
+  if (d->ld_act_d < d->d_model || d->ld_w < d->d_model) return FAIL(MECEFO_ERR_INVALID_ARG, "a row stride is smaller than the logical width");
+  if (!isfinite(d->logit_scale)) return FAIL(MECEFO_ERR_INVALID_ARG, "logit_scale must be finite");
+  h->d = d;
+  h->bf16 = d->dtype == MECEFO_BF16;
+  h->esz = h->bf16 ? 2 : 4;
+  if (h->bf16 && d->d_model % 8) return FAIL(MECEFO_ERR_UNSUPPORTED, "bf16 path needs d_model to be a multiple of 8 (got %d)", d->d_model);
+  if (h->bf16 && (d->ld_act_d % 8 || d->ld_w % 8)) return FAIL(MECEFO_ERR_INVALID_ARG, "bf16 path needs every row stride to be a multiple of 8 elements");
+  if (reaches_2gib(d->tokens, d->ld_act_d, h->esz) || reaches_2gib(d->vocab, d->ld_w, 4) || reaches_2gib(d->tokens, up(d->vocab, 8), 4))
+    return FAIL(MECEFO_ERR_UNSUPPORTED, "a tensor reaches 2 GiB; split the token batch");
+  h->b = (int)d->tokens;
+  h->dm = d->d_model;
+  h->vocab = d->vocab;
+  h->ldz = up(d->vocab, 8);
+  return MECEFO_OK;
+}
+
+mecefo_status_t check_ptr(const Head& h, const void* p, const char* name, bool required) {
+  if (!p) return required ? FAIL(MECEFO_ERR_INVALID_ARG, "%s is NULL", name) : MECEFO_OK;
+  if ((uintptr_t)p % (h.bf16 ? 16 : 4)) return FAIL(MECEFO_ERR_INVALID_ARG, "%s is not %d-byte aligned", name, h.bf16 ? 16 : 4);
+  return MECEFO_OK;
+}
+mecefo_status_t check_small(const void* p, const char* name, int align, bool required) {
+  if (!p) return required ? FAIL(MECEFO_ERR_INVALID_ARG, "%s is NULL", name) : MECEFO_OK;
+  if ((uintptr_t)p % align) return FAIL(MECEFO_ERR_INVALID_ARG, "%s is not %d-byte aligned", name, align);
+  return MECEFO_OK;
+}
+mecefo_status_t check_apart(const void* a, size_t na, const char* an, const void* b, size_t nb, const char* bn) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  if (a && b && na && nb && x < y + nb && y < x + na) return FAIL(MECEFO_ERR_INVALID_ARG, "%s overlaps %s", an, bn);
+  return MECEFO_OK;
+}
+
+// Parts of dU at most: the contraction over the vocabulary is long and its output small where there are few tokens.
+constexpr int kMaxParts = 16;
+constexpr int64_t kPartRoom = 32 << 20;      // fp32 elements
+
+struct HeadWs {
+  size_t U, rstd, Z, dZ, dU, part, dgp, zero, total;
+  int64_t room;
+};
+HeadWs layout(const Head& h, bool backward) {
+  HeadWs w;
+  size_t off = 0;
+  auto take = [&](int64_t bytes) { size_t o = off; off += (size_t)up(bytes, 256); return o; };
+  const int64_t act = (int64_t)h.b * h.dm;
+  w.U = take(act * h.esz);
+  w.rstd = take((int64_t)h.b * 4);
+  w.Z = take((int64_t)h.b * h.ldz * 4);
+  w.dZ = w.dU = w.part = w.dgp = w.zero = off;
+  w.room = 0;
+  if (backward) {
+    w.dZ = take((int64_t)h.b * h.ldz * h.esz);
+    w.dU = take(act * h.esz);
+    w.room = act * kMaxParts < kPartRoom ? act * kMaxParts : kPartRoom;
+    w.part = take(w.room * 4);
+    w.dgp = take((int64_t)rmsnorm_bwd_blocks(h.b) * h.dm * 4);
+    w.zero = take((int64_t)h.dm * h.esz);
+  }
+  w.total = off + 256;
+  return w;
+}
+mecefo_status_t carve(const Head& h, bool backward, void* ws, size_t ws_bytes, HeadWs* w, char** base) {
+  *w = layout(h, backward);
+  if (w->total > ws_bytes) return FAIL(MECEFO_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, w->total);
+  if (!ws) return FAIL(MECEFO_ERR_INVALID_ARG, "workspace is NULL");
+  *base = (char*)(((uintptr_t)ws + 255) / 256 * 256);
+  return MECEFO_OK;
+}
+
+GemmLaunch product(const Head& h, bool akc, bool bkc, int epi, const void* A, int64_t lda, const void* B, int64_t ldb, void* C,
+                   int64_t ldc, int M, int N, int K) {
+  GemmLaunch g;
+  memset(&g, 0, sizeof(g));
+  g.a_kcontig = akc;
+  g.b_kcontig = bkc;
+  g.epi = epi;
+  g.bf16 = h.bf16;
+  g.nprob = 1;
+  GemmProblem& p = g.p[0];
+  p.A[0] = p.A[1] = A;
+  p.B[0] = p.B[1] = B;
+  p.C[0] = C;
+  p.lda = lda; p.ldb = ldb; p.ldc = ldc;
+  p.M = M; p.N = N; p.K = K; p.nseg = 1;
+  return g;
+}
+
+// U, which is X where there is no gain.
+mecefo_status_t head_norm(const Head& h, const HeadWs& w, char* base, const void* X, const void* gamma, const void** U, int64_t* ldu,
+                          hipStream_t s) {
+  *U = X;
+  *ldu = h.d->ld_act_d;
+  if (!gamma) return MECEFO_OK;
+  HIP_TRY(launch_rmsnorm_fwd(h.bf16, X, h.d->ld_act_d, gamma, h.d->rms_eps, base + w.U, h.dm, (float*)(base + w.rstd), h.b, h.dm, s));
+  *U = base + w.U;
+  *ldu = h.dm;
+  return MECEFO_OK;
+}
+// The products z = U W^T in fp32.
+mecefo_status_t head_products(const Head& h, const HeadWs& w, char* base, const void* U, int64_t ldu, const void* W, hipStream_t s) {
+  GemmLaunch g = product(h, true, true, EPI_GRAD, U, ldu, W, h.d->ld_w, base + w.Z, h.ldz, h.b, h.vocab, h.dm);
+  g.out_f32 = true;
+  HIP_TRY(launch_gemm(g, s));
+  return MECEFO_OK;
+}
+
+}  // namespace
+}  // namespace mecefo
+
+using namespace mecefo;
+
+extern "C" {
+
+mecefo_status_t mecefo_head_workspace_bytes(const mecefo_head_desc_t* desc, int backward, size_t* out_bytes) {
+  Head h;
+  TRY(check_desc(desc, &h));
+  if (!out_bytes) return FAIL(MECEFO_ERR_INVALID_ARG, "out_bytes is NULL");
+  *out_bytes = layout(h, backward != 0).total;
+  return MECEFO_OK;
+}
+
+mecefo_status_t mecefo_head_logprob_fwd(const mecefo_head_desc_t* desc, const void* X, const void* gamma, const void* W,
+                                        const int64_t* labels, float* logp, float* lse, void* ws, size_t ws_bytes,
+                                        void* hip_stream) {
+  Head h;
+  TRY(check_desc(desc, &h));
+  const bool any = h.b > 0;
+  TRY(check_ptr(h, X, "X", any)); TRY(check_ptr(h, gamma, "gamma", false)); TRY(check_ptr(h, W, "W", true));
+  TRY(check_small(labels, "labels", 8, any)); TRY(check_small(logp, "logp", 4, any)); TRY(check_small(lse, "lse", 4, false));
+  HeadWs w;
+  char* base;
+  TRY(carve(h, false, ws, ws_bytes, &w, &base));
+  if (!any) return MECEFO_OK;
+  hipStream_t s = (hipStream_t)hip_stream;
+  const void* U;
+  int64_t ldu;
+  TRY(head_norm(h, w, base, X, gamma, &U, &ldu, s));
+  TRY(head_products(h, w, base, U, ldu, W, s));
+  hipLaunchKernelGGL(head_rows_kernel, dim3(h.b), dim3(256), 0, s, (const float*)(base + w.Z), h.ldz, h.vocab, desc->logit_scale, labels,
+                     logp, lse);
+  HIP_TRY(hipGetLastError());
+  return MECEFO_OK;
+}
+
+mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const void* X, const void* gamma, const void* W,
+                                        const int64_t* labels, const float* lse, const float* dlogp, void* dX, void* dgamma,
+                                        void* dW, int accumulate, void* ws, size_t ws_bytes, void* hip_stream) {
+  Head h;
+  TRY(check_desc(desc, &h));
+  const bool any = h.b > 0, grad_f32 = desc->grad_dtype == MECEFO_F32;
+  TRY(check_ptr(h, X, "X", any)); TRY(check_ptr(h, gamma, "gamma", false)); TRY(check_ptr(h, W, "W", true));
+  TRY(check_small(labels, "labels", 8, any)); TRY(check_small(lse, "lse", 4, any)); TRY(check_small(dlogp, "dlogp", 4, any));
+  TRY(check_ptr(h, dX, "dX", any)); TRY(check_ptr(h, dgamma, "dgamma", false)); TRY(check_ptr(h, dW, "dW", true));
+  if (dgamma && !gamma) return FAIL(MECEFO_ERR_INVALID_ARG, "dgamma requested but gamma is NULL");
+  const size_t act = any ? (size_t)((h.b - 1) * desc->ld_act_d + h.dm) * h.esz : 0, wt = (size_t)((h.vocab - 1) * desc->ld_w + h.dm);
+  TRY(check_apart(dX, act, "dX", X, act, "X")); TRY(check_apart(dX, act, "dX", W, wt * h.esz, "W"));
+  TRY(check_apart(dW, wt * (grad_f32 ? 4 : h.esz), "dW", W, wt * h.esz, "W")); TRY(check_apart(dW, wt * (grad_f32 ? 4 : h.esz), "dW", X, act, "X"));
+  TRY(check_apart(dW, wt * (grad_f32 ? 4 : h.esz), "dW", dX, act, "dX"));
+  HeadWs w;
+  char* base;
+  TRY(carve(h, true, ws, ws_bytes, &w, &base));
+  hipStream_t s = (hipStream_t)hip_stream;
+  const void* U = X;
+  int64_t ldu = desc->ld_act_d;
+  void* dZ = base + w.dZ;
+  if (any) {
+    TRY(head_norm(h, w, base, X, gamma, &U, &ldu, s));
+    TRY(head_products(h, w, base, U, ldu, W, s));
+    const float* Z = (const float*)(base + w.Z);
+    if (h.bf16) hipLaunchKernelGGL(head_dz_kernel<__bf16>, dim3(h.b), dim3(256), 0, s, Z, h.ldz, h.vocab, desc->logit_scale, labels, lse, dlogp, (__bf16*)dZ);
+    else hipLaunchKernelGGL(head_dz_kernel<float>, dim3(h.b), dim3(256), 0, s, Z, h.ldz, h.vocab, desc->logit_scale, labels, lse, dlogp, (float*)dZ);
+    HIP_TRY(hipGetLastError());
+  }
+  {  // dW = dz^T U   [V x d], contraction over tokens
+    GemmLaunch g = product(h, false, false, EPI_GRAD, dZ, h.ldz, U, ldu, dW, desc->ld_w, h.vocab, h.dm, h.b);
+    g.out_f32 = grad_f32;
+    g.accumulate = accumulate;
+    HIP_TRY(launch_gemm(g, s));
+  }
+  int nblk = 0;
+  float* dgp = (float*)(base + w.dgp);
+  if (any) {  // dU = dz W   [b x d], contraction over the vocabulary
+    void* dU = gamma ? base + w.dU : dX;
+    const int64_t lddu = gamma ? h.dm : desc->ld_act_d;
+    GemmLaunch g = product(h, true, false, EPI_STORE, dZ, h.ldz, W, desc->ld_w, dU, h.dm, h.b, h.dm, h.vocab);
+    g.p[0].kpad_ok = 1;      // dz has zeros behind the vocabulary
+    if (h.bf16) bf16_plan_splits(g, w.room);
+    else f32_plan_splits(g, (int)(w.room / ((int64_t)h.b * h.dm)));
+    const int parts = g.p[0].splits;
+    if (parts > 1) g.p[0].C[0] = base + w.part;
+    else g.p[0].ldc = lddu;
+    HIP_TRY(launch_gemm(g, s));
+    if (parts > 1) {
+      const float* part = (const float*)(base + w.part);
+      const unsigned grid = (unsigned)(((int64_t)h.b * h.dm + 255) / 256);
+      if (h.bf16) hipLaunchKernelGGL(head_sum_kernel<__bf16>, dim3(grid), dim3(256), 0, s, part, parts, (int64_t)h.b, h.dm, (__bf16*)dU, lddu);
+      else hipLaunchKernelGGL(head_sum_kernel<float>, dim3(grid), dim3(256), 0, s, part, parts, (int64_t)h.b, h.dm, (float*)dU, lddu);
+      HIP_TRY(hipGetLastError());
+    }
+    if (gamma) {  // dX = normbwd(dU): the norm backward adds a residual gradient, here a row of zeros with stride 0
+      const int words = (h.dm * h.esz + 3) / 4;
+      hipLaunchKernelGGL(head_zero_kernel, dim3((words + 255) / 256), dim3(256), 0, s, (uint32_t*)(base + w.zero), words);
+      HIP_TRY(hipGetLastError());
+      const NormBwd n = {dU, h.dm, 0, 0, X, desc->ld_act_d, (const float*)(base + w.rstd), gamma, base + w.zero, 0, dX, desc->ld_act_d,
+                         dgamma ? dgp : nullptr, (int64_t)rmsnorm_bwd_blocks(h.b) * h.dm, h.b, h.dm};
+      HIP_TRY(launch_rmsnorm_bwd(h.bf16, n, &nblk, s));
+    }
+  }
+  if (dgamma) HIP_TRY(launch_dgamma_reduce(dgp, nblk, h.dm, dgamma, grad_f32, h.bf16, accumulate, s));
+  return MECEFO_OK;
+}
+
+}  // extern "C"

@@ -212,6 +212,13 @@ hipError_t launch_attn_bwd_kv(const void* Q, const void* K, const void* V, int64
                               int64_t ldp, int batch, int seq, int heads, int dh, float scale, hipStream_t s);
 
 
+// 8-bit checkpoints (checkpoint.hip): bytes q [rows x ldq], 16-byte aligned, and one byte e per 32 columns [rows x lde].
+struct Ckpt { int8_t* q; uint8_t* e; int64_t ldq, lde; };
+bool reaches_2gib(int64_t rows, int64_t ld, int esz);
+hipError_t launch_ckpt_pack(bool bf16, const void* X, int64_t ldx, int64_t rows, int cols, const Ckpt& k, hipStream_t s);
+hipError_t launch_ckpt_unpack(bool bf16, const Ckpt& k, int64_t rows, int cols, void* X, int64_t ldx, hipStream_t s);
+
+
 // Fused causal attention forward: O = softmax(scale Q K^T) V and the row log-sum-exp L [batch*heads][seq],
 // no score or probability buffer.  Q, K, V, O token-major with row stride ld (elements), head h at
 // columns h*dh.  bf16, head dimension 64 or 128, ld a multiple of 8.

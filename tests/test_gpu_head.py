@@ -1,0 +1,213 @@
+"""LM head log-probabilities and their gradient against the oracle in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import training_oracle as T
+from paper_2510_16415_amd import binding as B
+from paper_2510_16415_amd import inputs as I
+from tests.gpu_util import dev, poisoned_ws, relerr, up8
+
+pytestmark = pytest.mark.gpu
+CODE = {"bf16": B.BF16, "f32": B.F32}
+U32 = 2.0 ** -24      # half a step of fp32
+# a norm-wise gate for the gradients.  bf16: dz is rounded once and the result once, at most 2^-8 of a value each; fp32: a
+# sum of K terms in another order, far below the gate of the fp32 path
+GATE = {"bf16": 2 * 2.0 ** -8, "f32": 1e-5}
+
+
+def case(b, d, v, dtype, seed=0, skip=0.2, std=0.2):
+    rng = np.random.default_rng([seed, b, d, v])
+    cast = (lambda x: I.round_to_bf16_grid(x)) if dtype == "bf16" else (lambda x: x.astype(np.float32))
+    X, W = cast(rng.standard_normal((b, d))), cast(rng.standard_normal((v, d)) * std)
+    labels = rng.integers(0, v, b)
+    labels[rng.random(b) < skip] = rng.choice([-1, -100, v, 1 << 40])
+    return X, W, labels.astype(np.int64), rng.standard_normal(b).astype(np.float32) / b
+
+
+def logp_bound(X, W, scale, v):
+    """Per row: two products of d terms added in fp32, each term's partial sums rounded at most d times; the sum of v
+    exponentials, added in chains of at most v / 32 + 200 positive terms; exp2 and log to a few units of fp32."""
+    size = abs(scale) * (np.abs(X.astype(np.float64)) @ np.abs(W.astype(np.float64)).T).max(axis=1)
+    return 2 * (X.shape[1] + 8) * U32 * size + (v / 32 + 260) * U32 + 8 * U32 * size
+
+
+def run_fwd(X, W, labels, dtype, scale=1.0, gamma=None, pad=0, lse=True, stream=None):
+    b, d, v = len(X), X.shape[1], len(W)
+    ld = d + pad
+    desc = B.make_head_desc(b, d, v, CODE[dtype], B.F32, ld, ld, scale)
+    logp, L = torch.full((b,), 9.0, device="cuda"), torch.full((b,), 9.0, device="cuda")
+    B.mecefo_head_logprob_fwd(desc, dev(X, dtype, ld), None if gamma is None else dev(gamma, dtype), dev(W, dtype, ld),
+                              torch.from_numpy(labels).cuda(), logp, L if lse else None,
+                              poisoned_ws(B.mecefo_head_workspace_bytes(desc, False)), stream)
+    return logp, L
+
+
+def run_bwd(X, W, labels, L, c, dtype, scale=1.0, gamma=None, pad=0, grad="f32", accumulate=0, fill=0.25):
+    b, d, v = len(X), X.shape[1], len(W)
+    ld = d + pad
+    gt, gcode = (torch.float32, B.F32) if grad == "f32" else (torch.bfloat16, B.BF16)
+    desc = B.make_head_desc(b, d, v, CODE[dtype], gcode, ld, ld, scale)
+    dX = torch.full((b, ld), 5.0, dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device="cuda")
+    dW = torch.full((v, ld), fill, dtype=gt, device="cuda")
+    dg = None if gamma is None else torch.full((d,), fill, dtype=gt, device="cuda")
+    B.mecefo_head_logprob_bwd(desc, dev(X, dtype, ld), None if gamma is None else dev(gamma, dtype), dev(W, dtype, ld),
+                              torch.from_numpy(labels).cuda(), L, torch.from_numpy(c).cuda(), dX, dg, dW, accumulate,
+                              poisoned_ws(B.mecefo_head_workspace_bytes(desc, True)))
+    if pad:
+        assert (dX[:, d:] == 5.0).all() and (dW[:, d:] == fill).all()
+    f = lambda t: t.float().cpu().numpy().astype(np.float64)      # noqa: E731
+    return f(dX[:, :d]), f(dW[:, :d]), None if dg is None else f(dg)
+
+
+SIZES = [(1, 8, 1), (1, 64, 7), (2, 16, 8), (3, 40, 33), (17, 64, 255), (64, 128, 257), (65, 256, 1000), (130, 72, 4099),
+         (300, 512, 2000), (1, 1024, 32000), (77, 256, 8191), (513, 64, 130)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("b,d,v", SIZES + [(257, 4096, 515)])
+def test_forward(b, d, v, dtype):
+    X, W, labels, _ = case(b, d, v, dtype)
+    logp, L = run_fwd(X, W, labels, dtype)
+    want, lse = T.head_fwd(X, W, labels)
+    tol = logp_bound(X, W, 1.0, v)
+    assert (np.abs(logp.cpu().numpy() - want) <= tol).all() and (np.abs(L.cpu().numpy() - lse) <= tol).all()
+    skipped = (labels < 0) | (labels >= v)
+    assert (logp.cpu().numpy()[skipped] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_forward_of_odd_width(dtype):
+    d = 24 if dtype == "bf16" else 13
+    X, W, labels, _ = case(9, d, 50, dtype)
+    logp, L = run_fwd(X, W, labels, dtype, pad=8 if dtype == "bf16" else 3, lse=False)
+    want, _ = T.head_fwd(X, W, labels)
+    assert (np.abs(logp.cpu().numpy() - want) <= logp_bound(X, W, 1.0, 50)).all() and (L == 9.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.25, -1.5, 0.0, 40.0])
+def test_scale_and_large_logits(dtype, scale):
+    X, W, labels, c = case(66, 128, 300, dtype, std=1.0)      # at 40: logits in the hundreds
+    logp, L = run_fwd(X, W, labels, dtype, scale)
+    want, lse = T.head_fwd(X, W, labels, scale)
+    tol = logp_bound(X, W, scale, 300)
+    assert (np.abs(logp.cpu().numpy() - want) <= tol).all() and (np.abs(L.cpu().numpy() - lse) <= tol).all()
+    dX, dW, _ = run_bwd(X, W, labels, L, c, dtype, scale)
+    wX, wW = T.head_bwd(X, W, labels, c, scale)
+    assert np.isfinite(dX).all() and np.isfinite(dW).all()
+    if scale == 0.0:
+        assert not dX.any() and not dW.any()
+    elif scale < 10:
+        assert relerr(dX, wX) <= GATE[dtype] and relerr(dW, wW) <= GATE[dtype]
+    else:      # a logit of size 3000 is known to 2 d U32 of that: exp() turns it into a relative error of the probabilities
+        more = 2 * tol.max()
+        assert relerr(dX, wX) <= GATE[dtype] + more and relerr(dW, wW) <= GATE[dtype] + more
+
+
+@pytest.mark.parametrize("dtype,grad", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("b,d,v", SIZES)
+def test_backward(b, d, v, dtype, grad):
+    X, W, labels, c = case(b, d, v, dtype, seed=1)
+    _, L = run_fwd(X, W, labels, dtype, pad=8)
+    dX, dW, _ = run_bwd(X, W, labels, L, c, dtype, pad=8, grad=grad)
+    wX, wW = T.head_bwd(X, W, labels, c)
+    if v == 1:      # one word: nothing to learn; the product and its log-sum-exp differ by a rounding
+        assert np.abs(dX).max() <= 1e-5 and np.abs(dW).max() <= 1e-5
+        return
+    assert relerr(dX, wX) <= GATE[dtype] and relerr(dW, wW) <= GATE[dtype]
+    skipped = (labels < 0) | (labels >= v)
+    assert not dX[skipped].any()
+
+
+@pytest.mark.parametrize("dtype,grad", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+def test_backward_adds_to_its_gradients(dtype, grad):
+    X, W, labels, c = case(130, 64, 500, dtype, seed=2)
+    gamma = np.ones(64, np.float32)
+    _, L = run_fwd(X, W, labels, dtype, gamma=gamma)
+    over = run_bwd(X, W, labels, L, c, dtype, gamma=gamma, grad=grad, accumulate=0)
+    more = run_bwd(X, W, labels, L, c, dtype, gamma=gamma, grad=grad, accumulate=1)
+    step = 2.0 ** -8 if grad == "bf16" else U32      # rounded once more
+    assert np.array_equal(over[0], more[0])
+    for a, m in zip(over[1:], more[1:]):
+        assert (np.abs(m - (a + 0.25)) <= step * (np.abs(a) + np.abs(m) + 0.25)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("b,d,v", [(1, 64, 40), (70, 256, 300), (300, 2048, 257), (2500, 128, 100), (40, 4104, 70)])
+def test_with_a_norm(b, d, v, dtype):
+    X, W, labels, c = case(b, d, v, dtype, seed=3, std=d ** -0.5)
+    rng = np.random.default_rng(4)
+    gamma = I.round_to_bf16_grid(1 + 0.2 * rng.standard_normal(d)) if dtype == "bf16" else (1 + 0.2 * rng.standard_normal(d)).astype(np.float32)
+    logp, L = run_fwd(X, W, labels, dtype, gamma=gamma)
+    x = X.astype(np.float64)
+    rs = 1 / np.sqrt((x * x).mean(axis=1, keepdims=True) + float(np.float32(1e-6)))
+    N = x * rs
+    U = N * gamma
+    if dtype == "bf16":
+        U = I.round_to_bf16_grid(U).astype(np.float64)
+    want, lse = T.head_fwd(U, W, labels)
+    # U is rounded by the kernel and by the oracle from values that differ in the last bits of fp32: now and then one of
+    # them goes to the next number, half a step of bf16 (fp32: a few units)
+    flip = (2.0 ** -8 if dtype == "bf16" else 8 * U32) * (np.abs(U) @ np.abs(W.astype(np.float64)).T).max(axis=1)
+    tol = logp_bound(U, W, 1.0, v) + 2 * flip
+    assert (np.abs(logp.cpu().numpy() - want) <= tol).all() and (np.abs(L.cpu().numpy() - lse) <= tol).all()
+    dX, dW, dg = run_bwd(X, W, labels, L, c, dtype, gamma=gamma)
+    dU, wW = T.head_bwd(U, W, labels, c)
+    dN = dU * gamma
+    wX = rs * (dN - N * (dN * N).mean(axis=1, keepdims=True))
+    # dz, dU and dX are rounded to bf16, 2^-8 each, and dz and dW see a U that is off as above
+    gate = 4 * 2.0 ** -8 if dtype == "bf16" else 1e-5
+    assert relerr(dX, wX) <= gate and relerr(dW, wW) <= gate and relerr(dg, (dU * N).sum(axis=0)) <= gate
+
+
+def test_tokens_that_are_not_scored_may_carry_anything_in_dlogp():
+    X, W, labels, c = case(50, 64, 90, "bf16", seed=5, skip=0.5)
+    skipped = (labels < 0) | (labels >= 90)
+    assert 0 < skipped.sum() < 50
+    _, L = run_fwd(X, W, labels, "bf16")
+    clean = run_bwd(X, W, labels, L, np.where(skipped, 0, c).astype(np.float32), "bf16")
+    dirty = run_bwd(X, W, labels, L, np.where(skipped, np.nan, c).astype(np.float32), "bf16")
+    assert np.array_equal(clean[0], dirty[0]) and np.array_equal(clean[1], dirty[1])
+    labels[:] = -1
+    none = run_bwd(X, W, labels, L, np.full(50, np.inf, np.float32), "bf16")
+    assert not none[0].any() and not none[1].any()
+
+
+def test_no_tokens_clear_or_keep_the_gradients():
+    for accumulate in (0, 1):
+        desc = B.make_head_desc(0, 64, 90, B.BF16)
+        dW, dg = torch.full((90, 64), 2.0, device="cuda"), torch.full((64,), 2.0, device="cuda")
+        W, gamma = torch.zeros(90, 64, dtype=torch.bfloat16, device="cuda"), torch.ones(64, dtype=torch.bfloat16, device="cuda")
+        B.mecefo_head_logprob_bwd(desc, None, gamma, W, None, None, None, None, dg, dW, accumulate,
+                                  poisoned_ws(B.mecefo_head_workspace_bytes(desc, True)))
+        assert (dW == 2.0 * accumulate).all() and (dg == 2.0 * accumulate).all()
+
+
+@pytest.mark.parametrize("tile", ["S", "S4", "T", "T2", "X", "L8", "LT", "K", "L4", "L8R"])
+def test_every_tile_gives_the_same_to_a_rounding(tile, mecefo_option):
+    X, W, labels, c = case(333, 192, 1111, "bf16", seed=6)
+    mecefo_option("tile", tile)
+    logp, L = run_fwd(X, W, labels, "bf16")
+    want, lse = T.head_fwd(X, W, labels)
+    tol = logp_bound(X, W, 1.0, 1111)
+    assert (np.abs(logp.cpu().numpy() - want) <= tol).all() and (np.abs(L.cpu().numpy() - lse) <= tol).all()
+    dX, dW, _ = run_bwd(X, W, labels, L, c, "bf16")
+    wX, wW = T.head_bwd(X, W, labels, c)
+    assert relerr(dX, wX) <= GATE["bf16"] and relerr(dW, wW) <= GATE["bf16"]
+
+
+def test_repeats_are_bit_equal_and_streams_do_not_mix():
+    X, W, labels, c = case(200, 256, 3000, "bf16", seed=7)
+    first = run_fwd(X, W, labels, "bf16")
+    grads = run_bwd(X, W, labels, first[1], c, "bf16")
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    for s in streams:
+        with torch.cuda.stream(s):
+            got.append(run_fwd(X, W, labels, "bf16", stream=s))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for g in got for a, b in zip(g, first))
+    again = run_bwd(X, W, labels, first[1], c, "bf16")
+    assert all(np.array_equal(a, b) for a, b in zip(grads[:2], again[:2]))
