@@ -247,6 +247,59 @@ template <class Cfg, int NS_, int KG_ = 1> struct DtlPipe {
   static_assert(NS >= 2 && NS <= 4 && LDS_BYTES <= 160 * 1024 && (NS - 1) * FPS <= 63, "bad pipeline");
 };
 
+// A lane's value combined over its 16-lane row, in all of them.
+template <class F> __device__ inline float row16(float v, F f) {
+  auto dpp = [](float x, auto ctrl) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, true));
+  };
+  v = f(v, dpp(v, std::integral_constant<int, 0xB1>{}));       // the neighbour, the other pair of the quad,
+  v = f(v, dpp(v, std::integral_constant<int, 0x4E>{}));
+  v = f(v, dpp(v, std::integral_constant<int, 0x141>{}));      // the other quad of the half, the other half
+  return f(v, dpp(v, std::integral_constant<int, 0x140>{}));
+}
+
+// EPI_HEAD_LSE of a wave's accumulators, without LDS: element e of block (i, j) is row 16 i + 4 (lane / 16) + e, column
+// 16 j + lane % 16 of the wave's part, so a row is TN values in each of 16 lanes.  The 4 TM rows of a lane are handed to its
+// 16-lane row, one to a lane, and 16 of them go out in one store.
+template <int TM, int TN>
+__device__ inline void head_lse(const GemmProblem& p, const f32x4_t (&acc)[TM][TN], int row_w, int col_w, int lane) {
+  if (col_w >= p.N) return;
+  const int64_t* labels = (const int64_t*)p.C[1];
+  float2* out = (float2*)p.C[0] + (int64_t)(col_w / (16 * TN)) * p.ldc;
+  const int c0 = lane & 15, left = p.N - col_w;
+#pragma unroll
+  for (int i0 = 0; i0 < TM; i0 += 4) {
+    float2 mine = {0.f, 0.f};
+#pragma unroll
+    for (int i = i0; i < TM && i < i0 + 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float z[TN], m = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          z[j] = 16 * j + c0 < left ? acc[i][j][e] * p.scale : -INFINITY;
+          m = fmaxf(m, z[j]);
+        }
+        m = row16(m, [](float a, float b) { return fmaxf(a, b); });
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) s += __builtin_amdgcn_exp2f(1.44269504088896341f * (z[j] - m));
+        s = row16(s, [](float a, float b) { return a + b; });
+        if (c0 == 4 * (i - i0) + e) mine = float2{m, s};
+        const int row = row_w + 16 * i + 4 * (lane >> 4) + e;
+        const int64_t at = (row < p.M ? labels[row] : -1) - col_w;
+        if (at >= 0 && at < left && at < 16 * TN && (int)(at & 15) == c0) {      // one lane of the launch
+          float zl = z[0];
+#pragma unroll
+          for (int j = 1; j < TN; ++j) zl = (int)(at >> 4) == j ? z[j] : zl;
+          ((float*)p.C[2])[row] = zl;
+        }
+      }
+    const int row = row_w + 16 * (i0 + (c0 >> 2)) + 4 * (lane >> 4) + (c0 & 3);
+    if (i0 + (c0 >> 2) < TM && row < p.M) out[row] = mine;
+  }
+}
+
 // RAGGED: K may end inside a 16-byte chunk (the instantiation without it keeps the large tile's loop free of the
 // test: 0.5 % of the 7B-shaped layer).
 // SEGS: products may have several K segments.
@@ -439,6 +492,10 @@ __device__ __forceinline__ void dtl_tile(const KHead& head, GemmProblem p, int m
         for (int j = 0; j < TN; ++j) acc[i][j] += part[(((g - 1) * TM + i) * TN + j) * NT + t];
   }
 
+  if constexpr (EPI == EPI_HEAD_LSE) {
+    head_lse<TM, TN>(p, acc, m0 + wm * Cfg::WM, n0 + wn * Cfg::WN, lane);
+    return;      // nothing behind this is reached
+  }
   fold_norm<EPI>(p, lane);
   // Epilogue, staged through LDS so that global accesses are 16 bytes per lane and cover whole
   // rows (bf16: eight columns per access, fp32: two accesses of four).  Accumulator element e of a 16x16 block sits at row
@@ -509,7 +566,7 @@ __device__ __forceinline__ void dtl_tile(const KHead& head, GemmProblem p, int m
             for (int e = 0; e < 4; ++e) { v2[e] = z0[e]; v2[4 + e] = z1[e]; }
           }
         }
-        if constexpr (!F32_OUT) epilogue_vec8<EPI>(p, head, split, row_w + i * 32 + rl, col_w, v, v2);
+        if constexpr (!F32_OUT && EPI != EPI_HEAD_LSE) epilogue_vec8<EPI>(p, head, split, row_w + i * 32 + rl, col_w, v, v2);
       }
     }
   }

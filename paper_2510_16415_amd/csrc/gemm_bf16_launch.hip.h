@@ -84,11 +84,11 @@ inline const TileModel& tile_model(int c) {
 // What the 192-row tile and the cut-up last round are built for: operands whose rows can be cut anywhere, and the
 // epilogues of launches that can be large.
 constexpr bool has_tile_k(bool akc, bool bkc, int epi) {
-  return akc && (epi == EPI_STORE || (bkc && (epi == EPI_GRAD || epi == EPI_SWIGLU_FWD || epi == EPI_SWIGLU_BWD || epi == EPI_RESID)));
+  return akc && (epi == EPI_STORE || (bkc && (epi == EPI_GRAD || epi == EPI_SWIGLU_FWD || epi == EPI_SWIGLU_BWD || epi == EPI_RESID || epi == EPI_HEAD_LSE || epi == EPI_HEAD_GRAD)));
 }
 constexpr bool has_tile_x(int epi) { return epi != EPI_ATTN_P && epi != EPI_ATTN_DS && epi != EPI_ROPE; }
 constexpr bool has_tail(bool akc, bool bkc, int epi) {
-  return has_tile_k(akc, bkc, epi) || (!akc && !bkc && (epi == EPI_GRAD || epi == EPI_STORE));
+  return (has_tile_k(akc, bkc, epi) && epi != EPI_HEAD_LSE) || (!akc && !bkc && (epi == EPI_GRAD || epi == EPI_STORE));
 }
 
 // K stages of a workgroup of problem i, and the workgroups of the problem on bm x bn tiles.
@@ -313,6 +313,7 @@ hipError_t run_bf16(GemmLaunch& g, hipStream_t stream) {
   constexpr bool DUAL = epi_is_dual(EPI);
   KArgs a;
   fill_kargs(a, g, Cfg::BM, DUAL ? Cfg::BN / 2 : Cfg::BN, kBK);
+  g.part_cols = Cfg::WN;
   if (a.h.total == 0) return hipSuccess;
   const hipError_t e = Kern::prepare();
   if (e != hipSuccess) return e;
@@ -355,9 +356,11 @@ hipError_t run_bf16_tail(GemmLaunch& g, const TailPlan& plan, hipStream_t stream
 }
 
 // The register-staged kernels serve as a second implementation in tests only; the epilogues of the projection refresh,
-// the residual adds and the rotation are not built for them, and such launches take the 256 x 256 direct-to-LDS tile
+// the residual adds, the rotation and the head are not built for them, and such launches take the 256 x 256 direct-to-LDS tile
 // where a register-staged one is forced.
-constexpr bool register_staged(int epi) { return epi != EPI_POLY && epi != EPI_HILO && epi != EPI_RESID && epi != EPI_ROPE; }
+constexpr bool register_staged(int epi) {
+  return epi != EPI_POLY && epi != EPI_HILO && epi != EPI_RESID && epi != EPI_ROPE && epi != EPI_HEAD_LSE && epi != EPI_HEAD_GRAD;
+}
 
 // Limit raise for the configurations of one (layout, epilogue) pair.
 template <bool AKC, bool BKC, int EPI>

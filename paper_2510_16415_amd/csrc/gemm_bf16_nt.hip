@@ -101,6 +101,8 @@ hipError_t launch_gemm_bf16_nt(GemmLaunch& g, hipStream_t s) {
     case EPI_HILO: return run_bf16_auto<true, true, EPI_HILO>(g, s);
     case EPI_RESID: return run_bf16_auto<true, true, EPI_RESID>(g, s);
     case EPI_ROPE: return run_rope(g, s);
+    case EPI_HEAD_LSE: return run_bf16_auto<true, true, EPI_HEAD_LSE>(g, s);
+    case EPI_HEAD_GRAD: return run_bf16_auto<true, true, EPI_HEAD_GRAD>(g, s);
     default: return hipErrorInvalidValue;
   }
 }
@@ -115,6 +117,8 @@ hipError_t prepare_gemm_bf16_nt() {
   if (e == hipSuccess) e = prepare_bf16<true, true, EPI_POLY>();
   if (e == hipSuccess) e = prepare_bf16<true, true, EPI_HILO>();
   if (e == hipSuccess) e = prepare_bf16<true, true, EPI_RESID>();
+  if (e == hipSuccess) e = prepare_bf16<true, true, EPI_HEAD_LSE>();
+  if (e == hipSuccess) e = prepare_bf16<true, true, EPI_HEAD_GRAD>();
   if (e == hipSuccess) e = PairKernel<CfgM, PipeM2>::prepare();
   if (e == hipSuccess) e = PairKernel<CfgM8, PipeM4>::prepare();
   if (e == hipSuccess) e = PairKernel<CfgT, PipeT>::prepare();

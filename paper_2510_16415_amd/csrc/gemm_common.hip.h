@@ -353,6 +353,14 @@ template <bool PRECISE> __device__ inline float sigmoid_f(float g) {
 
 template <int EPI> constexpr bool kUnhandledEpilogue = false;
 
+// EPI_HEAD_GRAD: what a row's gradients are made of; c = 0 where the row has no label among the columns.
+struct HeadRow { float c, lse; int label; };
+__device__ inline HeadRow head_row(const GemmProblem& p, int row) {
+  const int64_t label = ((const int64_t*)p.C[1])[row];
+  const bool counted = label >= 0 && label < p.N;
+  return HeadRow{counted ? p.addend[row] * p.scale : 0.f, p.rowvec[row], counted ? (int)label : -1};
+}
+
 // 1 / sqrt of a squared norm; a zero matrix is left unchanged.
 __device__ inline float inv_norm(float sq) { return sq > 0.f ? 1.0f / sqrtf(sq) : 1.0f; }
 // From the norms of the kNormBlocks parts of a matrix; every wave for itself, in a fixed order.
@@ -405,6 +413,16 @@ __device__ inline void epilogue_elem(const GemmProblem& p, const KHead& a, int s
       T* c = (T*)p.C[0] + (int64_t)row * p.ldc + col;
       *c = from_f32<T>(to_f32<T>(*c) * (v - p.rowvec[row]) * p.scale);
     }
+  } else if constexpr (EPI == EPI_HEAD_GRAD) {
+    constexpr bool PRECISE = sizeof(T) == 4;
+    if (col >= p.N && col >= p.pad_cols) return;
+    const HeadRow h = head_row(p, row);
+    float g = 0.f;
+    if (col < p.N && h.c != 0.f) {
+      const float x = v * p.scale - h.lse;
+      g = h.c * ((h.label == col ? 1.f : 0.f) - (PRECISE ? expf(x) : __builtin_amdgcn_exp2f(1.44269504088896341f * x)));
+    }
+    ((T*)p.C[0])[(int64_t)row * p.ldc + col] = from_f32<T>(g);
   } else if constexpr (EPI == EPI_RESID) {
     if (col < p.N) {
       const int64_t idx = (int64_t)row * p.ldc + col;
@@ -518,6 +536,15 @@ __device__ inline void epilogue_vec8(const GemmProblem& p, const KHead& a, int s
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = (float)pr[e] * (v[e] - dsum) * p.scale;
     *c = pack_bf16x8(o);
+  } else if constexpr (EPI == EPI_HEAD_GRAD) {
+    const HeadRow h = head_row(p, row);
+    float o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float pr = __builtin_amdgcn_exp2f(1.44269504088896341f * (v[e] * p.scale - h.lse));
+      o[e] = h.c == 0.f ? 0.f : h.c * ((h.label == col0 + e ? 1.f : 0.f) - pr);
+    }
+    *(bf16x8s_t*)((__bf16*)p.C[0] + idx) = pack_bf16x8(o);
   } else if constexpr (EPI == EPI_GRAD) {      // bf16 gradients; fp32 ones take epilogue_vec4
     bf16x8s_t* c = (bf16x8s_t*)((__bf16*)p.C[0] + idx);
     float o[8];

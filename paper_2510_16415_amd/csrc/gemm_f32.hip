@@ -421,7 +421,7 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_direct_kernel(const KArgs arg
   sum_quarters<EPI>(p, head, tc.split, m0, n0, t, acc, (float*)smem);
 }
 
-constexpr bool f32_nt_only(int epi) { return epi_is_dual(epi) || epi == EPI_ATTN_P || epi == EPI_ATTN_DS; }
+constexpr bool f32_nt_only(int epi) { return epi_is_dual(epi) || epi == EPI_ATTN_P || epi == EPI_ATTN_DS || epi == EPI_HEAD_GRAD; }
 
 // Workgroups of a launch with ft x ft tiles.
 inline int f32_tiles(const GemmLaunch& g, int ft) {
@@ -590,7 +590,7 @@ void f32_plan_splits(GemmLaunch& g, int most) {
 }
 
 hipError_t prepare_gemm_f32() {
-  return prepare_f32<EPI_STORE, EPI_GRAD, EPI_SWIGLU_FWD, EPI_SWIGLU_BWD, EPI_ATTN_P, EPI_ATTN_DS, EPI_POLY, EPI_HILO, EPI_RESID>();
+  return prepare_f32<EPI_STORE, EPI_GRAD, EPI_SWIGLU_FWD, EPI_SWIGLU_BWD, EPI_ATTN_P, EPI_ATTN_DS, EPI_POLY, EPI_HILO, EPI_RESID, EPI_HEAD_GRAD>();
 }
 
 hipError_t launch_gemm_f32(GemmLaunch& g, hipStream_t s) {
@@ -604,6 +604,7 @@ hipError_t launch_gemm_f32(GemmLaunch& g, hipStream_t s) {
     case EPI_POLY: return run_f32<EPI_POLY>(g, s);
     case EPI_HILO: return run_f32<EPI_HILO>(g, s);
     case EPI_RESID: return run_f32<EPI_RESID>(g, s);
+    case EPI_HEAD_GRAD: return run_f32<EPI_HEAD_GRAD>(g, s);
     default: return hipErrorInvalidValue;
   }
 }

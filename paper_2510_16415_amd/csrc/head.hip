@@ -43,18 +43,32 @@ __global__ __launch_bounds__(256) void head_rows_kernel(const float* __restrict_
   if (lse) lse[row] = l;
 }
 
-// dz of a row from its products, zeros behind the vocabulary.
-template <typename T>
-__global__ __launch_bounds__(256) void head_dz_kernel(const float* __restrict__ Z, int64_t ldz, int vocab, float scale,
-                                                      const int64_t* __restrict__ labels, const float* __restrict__ lse,
-                                                      const float* __restrict__ dlogp, T* __restrict__ dZ) {
-  const int64_t row = blockIdx.x;
-  const int64_t label = labels[row];
-  const float c = counted(label, vocab) ? dlogp[row] * scale : 0.f, l = lse[row];
-  const float* z = Z + row * ldz;
-  T* o = dZ + row * ldz;
-  for (int v = threadIdx.x; v < (int)ldz; v += 256)
-    o[v] = (T)(v < vocab && c != 0.f ? c * ((v == (int)label ? 1.f : 0.f) - expf(z[v] * scale - l)) : 0.f);
+// lse and logp from the parts that the products' epilogue leaves: (largest z, sum of exp(z - that)) of a row over part_cols
+// columns, [parts][rows], and z at the label.  16 rows to a workgroup, 64 threads share out a row's parts.
+__global__ __launch_bounds__(1024) void head_parts_kernel(const float2* __restrict__ part, int parts, int rows, int vocab,
+                                                          const float* __restrict__ zl, const int64_t* __restrict__ labels,
+                                                          float* __restrict__ logp, float* __restrict__ lse) {
+  __shared__ float2 red[64][16];
+  const int r = threadIdx.x & 15, g = threadIdx.x >> 4, row = blockIdx.x * 16 + r;
+  float2 a = {-INFINITY, 0.f};
+  auto join = [](float2 x, float2 y) {      // a part without columns is (-inf, 0)
+    const float m = fmaxf(x.x, y.x);
+    return m == -INFINITY ? float2{m, x.y + y.y} : float2{m, x.y * expf(x.x - m) + y.y * expf(y.x - m)};
+  };
+  if (row < rows) {
+#pragma unroll 4
+    for (int k = g; k < parts; k += 64) a = join(a, part[(int64_t)k * rows + row]);
+  }
+  red[g][r] = a;
+  __syncthreads();
+  for (int n = 32; n > 0; n >>= 1) {
+    if (g < n) red[g][r] = join(red[g][r], red[g + n][r]);
+    __syncthreads();
+  }
+  if (g != 0 || row >= rows) return;
+  const float l = red[0][r].x + logf(red[0][r].y);
+  logp[row] = counted(labels[row], vocab) ? zl[row] - l : 0.f;
+  if (lse) lse[row] = l;
 }
 
 // out[row, 0 .. cols) = sum of the parts [k][row, col], in their order.
@@ -99,7 +113,7 @@ mecefo_status_t check_desc(const mecefo_head_desc_t* d, Head* h) {
   h->esz = h->bf16 ? 2 : 4;
   if (h->bf16 && d->d_model % 8) return FAIL(MECEFO_ERR_UNSUPPORTED, "bf16 path needs d_model to be a multiple of 8 (got %d)", d->d_model);
   if (h->bf16 && (d->ld_act_d % 8 || d->ld_w % 8)) return FAIL(MECEFO_ERR_INVALID_ARG, "bf16 path needs every row stride to be a multiple of 8 elements");
-  if (reaches_2gib(d->tokens, d->ld_act_d, h->esz) || reaches_2gib(d->vocab, d->ld_w, 4) || reaches_2gib(d->tokens, up(d->vocab, 8), 4))
+  if (reaches_2gib(d->tokens, d->ld_act_d, h->esz) || reaches_2gib(d->vocab, d->ld_w, 4) || reaches_2gib(d->tokens, up(d->vocab, 8), h->esz))
     return FAIL(MECEFO_ERR_UNSUPPORTED, "a tensor reaches 2 GiB; split the token batch");
   h->b = (int)d->tokens;
   h->dm = d->d_model;
@@ -129,7 +143,7 @@ constexpr int kMaxParts = 16;
 constexpr int64_t kPartRoom = 32 << 20;      // fp32 elements
 
 struct HeadWs {
-  size_t U, rstd, Z, dZ, dU, part, dgp, zero, total;
+  size_t U, rstd, Z, zl, dZ, dU, part, dgp, zero, total;
   int64_t room;
 };
 HeadWs layout(const Head& h, bool backward) {
@@ -139,9 +153,12 @@ HeadWs layout(const Head& h, bool backward) {
   const int64_t act = (int64_t)h.b * h.dm;
   w.U = take(act * h.esz);
   w.rstd = take((int64_t)h.b * 4);
-  w.Z = take((int64_t)h.b * h.ldz * 4);
-  w.dZ = w.dU = w.part = w.dgp = w.zero = off;
+  w.Z = w.zl = w.dZ = w.dU = w.part = w.dgp = w.zero = off;
   w.room = 0;
+  if (!backward) {      // bf16: the parts of the log-sum-exps, over 32 columns where the tiles are the smallest; fp32: the products
+    w.Z = take(h.bf16 ? ((int64_t)h.vocab + 31) / 32 * h.b * 8 : (int64_t)h.b * h.ldz * 4);
+    w.zl = take((int64_t)h.b * 4);
+  }
   if (backward) {
     w.dZ = take((int64_t)h.b * h.ldz * h.esz);
     w.dU = take(act * h.esz);
@@ -190,13 +207,6 @@ mecefo_status_t head_norm(const Head& h, const HeadWs& w, char* base, const void
   *ldu = h.dm;
   return MECEFO_OK;
 }
-// The products z = U W^T in fp32.
-mecefo_status_t head_products(const Head& h, const HeadWs& w, char* base, const void* U, int64_t ldu, const void* W, hipStream_t s) {
-  GemmLaunch g = product(h, true, true, EPI_GRAD, U, ldu, W, h.d->ld_w, base + w.Z, h.ldz, h.b, h.vocab, h.dm);
-  g.out_f32 = true;
-  HIP_TRY(launch_gemm(g, s));
-  return MECEFO_OK;
-}
 
 }  // namespace
 }  // namespace mecefo
@@ -229,9 +239,20 @@ mecefo_status_t mecefo_head_logprob_fwd(const mecefo_head_desc_t* desc, const vo
   const void* U;
   int64_t ldu;
   TRY(head_norm(h, w, base, X, gamma, &U, &ldu, s));
-  TRY(head_products(h, w, base, U, ldu, W, s));
-  hipLaunchKernelGGL(head_rows_kernel, dim3(h.b), dim3(256), 0, s, (const float*)(base + w.Z), h.ldz, h.vocab, desc->logit_scale, labels,
-                     logp, lse);
+  GemmLaunch g = product(h, true, true, h.bf16 ? EPI_HEAD_LSE : EPI_STORE, U, ldu, W, desc->ld_w, base + w.Z,
+                         h.bf16 ? h.b : h.ldz, h.b, h.vocab, h.dm);
+  if (h.bf16) {
+    g.p[0].C[1] = const_cast<int64_t*>(labels);
+    g.p[0].C[2] = base + w.zl;
+    g.p[0].scale = desc->logit_scale;
+  }
+  HIP_TRY(launch_gemm(g, s));
+  if (h.bf16)
+    hipLaunchKernelGGL(head_parts_kernel, dim3((h.b + 15) / 16), dim3(1024), 0, s, (const float2*)(base + w.Z), cdiv(h.vocab, g.part_cols),
+                       h.b, h.vocab, (const float*)(base + w.zl), labels, logp, lse);
+  else
+    hipLaunchKernelGGL(head_rows_kernel, dim3(h.b), dim3(256), 0, s, (const float*)(base + w.Z), h.ldz, h.vocab, desc->logit_scale, labels,
+                       logp, lse);
   HIP_TRY(hipGetLastError());
   return MECEFO_OK;
 }
@@ -259,11 +280,14 @@ mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const vo
   void* dZ = base + w.dZ;
   if (any) {
     TRY(head_norm(h, w, base, X, gamma, &U, &ldu, s));
-    TRY(head_products(h, w, base, U, ldu, W, s));
-    const float* Z = (const float*)(base + w.Z);
-    if (h.bf16) hipLaunchKernelGGL(head_dz_kernel<__bf16>, dim3(h.b), dim3(256), 0, s, Z, h.ldz, h.vocab, desc->logit_scale, labels, lse, dlogp, (__bf16*)dZ);
-    else hipLaunchKernelGGL(head_dz_kernel<float>, dim3(h.b), dim3(256), 0, s, Z, h.ldz, h.vocab, desc->logit_scale, labels, lse, dlogp, (float*)dZ);
-    HIP_TRY(hipGetLastError());
+    GemmLaunch g = product(h, true, true, EPI_HEAD_GRAD, U, ldu, W, desc->ld_w, dZ, h.ldz, h.b, h.vocab, h.dm);
+    GemmProblem& p = g.p[0];
+    p.C[1] = const_cast<int64_t*>(labels);
+    p.pad_cols = (int)h.ldz;
+    p.rowvec = lse;
+    p.addend = dlogp;
+    p.scale = desc->logit_scale;
+    HIP_TRY(launch_gemm(g, s));
   }
   {  // dW = dz^T U   [V x d], contraction over tokens
     GemmLaunch g = product(h, false, false, EPI_GRAD, dZ, h.ldz, U, ldu, dW, desc->ld_w, h.vocab, h.dm, h.b);

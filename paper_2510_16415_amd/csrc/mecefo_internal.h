@@ -19,6 +19,10 @@ enum Epilogue : int {
                        // fold_norm (bf16): x = acc / (norm of a matrix whose kNormBlocks parts have the norms in rowvec)
   EPI_RESID = 9,       // C0[row, col] = acc + C1[row, col]   (activation dtype; C1 may be C0)
   EPI_ROPE = 10,       // C0 = acc rotated: pairs (j, j + rope_half) of every head by the angle of position row % rope_seq
+  EPI_HEAD_LSE = 11,   // z = scale * acc is not stored: C0 (fp32 pairs [columns / part_cols][ldc]) = the largest z of a row over part_cols
+                       // columns and the sum of exp(z - that); C2 (fp32) [row] = z at the row's label, C1 (int64)   (bf16, NT)
+  EPI_HEAD_GRAD = 12,  // C0[row, col] = scale * addend[row] * ([col = label] - exp(scale * acc - rowvec[row])), 0 where the label C1[row]
+                       // (int64) is no column; columns [N, pad_cols) are set to zero   (NT)
 };
 
 constexpr int kMaxProblems = 4;   // of one launch
@@ -44,7 +48,7 @@ struct GemmProblem {
   int64_t lda, ldb, ldc;
   int M, N, K;
   int nseg;        // 1 to 3 K segments (ignored for dual products)
-  int pad_cols;    // SwiGLU epilogues: columns [N, pad_cols) of the outputs are set to zero
+  int pad_cols;    // SwiGLU epilogues, EPI_HEAD_GRAD: columns [N, pad_cols) of the outputs are set to zero
   int kpad_ok;     // K-contiguous operands: bytes between K and the next multiple of 8 are known to be zero
   int splits;      // EPI_STORE: parts the contraction is cut into (0, 1: whole)
   bool whole;      // host side: never cut (the sum of the parts writes rows of ldc elements, padding included)
@@ -55,9 +59,9 @@ struct GemmProblem {
   // offsets are counted in operand elements (an fp32 output behind bf16 operands counts two per element).
   int batch, batch_inner;
   int64_t a_bo, a_bi, b_bo, b_bi, c_bo, c_bi;
-  const float* rowvec;   // attention epilogues: fp32 per output row, product z starts at z * M
-  float scale;           // attention epilogues, EPI_POLY
-  const float* addend;   // EPI_POLY, EPI_HILO: fp32 [M x ldc], may be NULL (zero); may be C0 of EPI_HILO itself
+  const float* rowvec;   // attention epilogues, EPI_HEAD_GRAD: fp32 per output row, product z starts at z * M
+  float scale;           // attention and head epilogues, EPI_POLY
+  const float* addend;   // EPI_POLY, EPI_HILO: fp32 [M x ldc], may be NULL (zero); may be C0 of EPI_HILO itself; EPI_HEAD_GRAD: [M]
   float poly_a, poly_b;  // EPI_POLY
   bool fold_norm;        // EPI_HILO: see there
   int rope_half, rope_seq;   // EPI_ROPE: half the head dimension (0: plain store) and the sequence length; rowvec and
@@ -95,6 +99,7 @@ struct GemmLaunch {
   int tile;         // EPI_ROPE: the configuration that gemm_bf16_rope_tile found for this launch
   SideJob side;
   bool side_done;   // set by the launcher: the side job is part of the launch
+  int part_cols;    // EPI_HEAD_LSE, set by the launcher: columns of a part, which depend on the tile
   uint32_t* clk;    // measurement: 64 (cycles, wall ticks) pairs written by the direct-to-LDS kernel, or NULL
 };
 
