@@ -434,6 +434,11 @@ def mecefo_projection_refresh(dtype, W, m, n, ldw, left, V0, ldv, r, power_iters
                                            cond_steps, polish_steps, _ptr(P), ldp, p, nb, _stream(stream)))
 
 
+def _at(t):
+    """A tensor's address as the argument types take it: calls of a few microseconds."""
+    return None if t is None else t.data_ptr()
+
+
 def ckpt(q, e) -> Ckpt:
     """Checkpoint argument from q [rows x >= 32 * groups] (int8) and e [rows x >= groups] (uint8), groups = ceil(cols / 32).
     The struct holds raw device pointers; it also keeps references to the tensors."""
@@ -447,11 +452,11 @@ def _kref(k):
 
 
 def mecefo_checkpoint_pack(dtype, X, rows, cols, ldx, ckpt, stream=None):
-    _check(lib().mecefo_checkpoint_pack(dtype, _ptr(X), rows, cols, ldx, _kref(ckpt), _stream(stream)))
+    _check(lib().mecefo_checkpoint_pack(dtype, _at(X), rows, cols, ldx, _kref(ckpt), _stream(stream)))
 
 
 def mecefo_checkpoint_unpack(dtype, ckpt, rows, cols, X, ldx, stream=None):
-    _check(lib().mecefo_checkpoint_unpack(dtype, _kref(ckpt), rows, cols, _ptr(X), ldx, _stream(stream)))
+    _check(lib().mecefo_checkpoint_unpack(dtype, _kref(ckpt), rows, cols, _at(X), ldx, _stream(stream)))
 
 
 def mecefo_block_ckpt_workspace_bytes(desc, r_gate=0, r_up=0, r_down=0) -> int:
@@ -465,9 +470,9 @@ def mecefo_block_bwd_skip_ckpt(desc, H, dOut, gamma, Wg, Wu, Wd, Pg, Pu, Pd, sid
     """H, G, Z: ckpt(...) arguments."""
     p, n = _ws(ws)
     null = Proj(None, 0, 0)
-    _check(lib().mecefo_block_bwd_skip_ckpt(C.byref(desc), _kref(H), _ptr(dOut), _ptr(gamma), _ptr(Wg), _ptr(Wu), _ptr(Wd),
+    _check(lib().mecefo_block_bwd_skip_ckpt(C.byref(desc), _kref(H), _at(dOut), _at(gamma), _at(Wg), _at(Wu), _at(Wd),
                                             Pg or null, Pu or null, Pd or null, int(side), _kref(G), _kref(Z),
-                                            exact_wgrad_mask, _ptr(dX), _ptr(dgamma), _ptr(dWg), _ptr(dWu), _ptr(dWd),
+                                            exact_wgrad_mask, _at(dX), _at(dgamma), _at(dWg), _at(dWu), _at(dWd),
                                             int(accumulate), p, n, _stream(stream)))
 
 
@@ -487,14 +492,14 @@ def mecefo_stack_ckpt_workspace_bytes(desc, attn, r_gate=0, r_up=0, r_down=0) ->
 def mecefo_stack_fwd_neighbor_ckpt(desc, attn, layers, X0, H, X_out, ws, stream=None):
     """H: ckpt_array(...)."""
     p, n = _ws(ws)
-    _check(lib().mecefo_stack_fwd_neighbor_ckpt(C.byref(desc), C.byref(attn), len(layers), layers, _ptr(X0), H, _ptr(X_out),
+    _check(lib().mecefo_stack_fwd_neighbor_ckpt(C.byref(desc), C.byref(attn), len(layers), layers, _at(X0), H, _at(X_out),
                                                 p, n, _stream(stream)))
 
 
 def mecefo_stack_bwd_skip_ckpt(desc, layers, H, lowrank, side, dOut_top, dX_bottom, accumulate, ws, stream=None):
     p, n = _ws(ws)
-    _check(lib().mecefo_stack_bwd_skip_ckpt(C.byref(desc), len(layers), layers, H, lowrank, int(side), _ptr(dOut_top),
-                                            _ptr(dX_bottom), int(accumulate), p, n, _stream(stream)))
+    _check(lib().mecefo_stack_bwd_skip_ckpt(C.byref(desc), len(layers), layers, H, lowrank, int(side), _at(dOut_top),
+                                            _at(dX_bottom), int(accumulate), p, n, _stream(stream)))
 
 
 def make_head_desc(tokens, d_model, vocab, dtype, grad_dtype=F32, ld_act_d=None, ld_w=None, logit_scale=1.0,
@@ -510,14 +515,14 @@ def mecefo_head_workspace_bytes(desc: HeadDesc, backward) -> int:
 
 def mecefo_head_logprob_fwd(desc, X, gamma, W, labels, logp, lse, ws, stream=None):
     p, n = _ws(ws)
-    _check(lib().mecefo_head_logprob_fwd(C.byref(desc), _ptr(X), _ptr(gamma), _ptr(W), _ptr(labels), _ptr(logp), _ptr(lse),
+    _check(lib().mecefo_head_logprob_fwd(C.byref(desc), _at(X), _at(gamma), _at(W), _at(labels), _at(logp), _at(lse),
                                          p, n, _stream(stream)))
 
 
 def mecefo_head_logprob_bwd(desc, X, gamma, W, labels, lse, dlogp, dX, dgamma, dW, accumulate, ws, stream=None):
     p, n = _ws(ws)
-    _check(lib().mecefo_head_logprob_bwd(C.byref(desc), _ptr(X), _ptr(gamma), _ptr(W), _ptr(labels), _ptr(lse), _ptr(dlogp),
-                                         _ptr(dX), _ptr(dgamma), _ptr(dW), int(accumulate), p, n, _stream(stream)))
+    _check(lib().mecefo_head_logprob_bwd(C.byref(desc), _at(X), _at(gamma), _at(W), _at(labels), _at(lse), _at(dlogp),
+                                         _at(dX), _at(dgamma), _at(dW), int(accumulate), p, n, _stream(stream)))
 
 
 def make_preference_desc(tokens, pairs, beta=0.1, label_smoothing=0.0, margin=0.0, length_mean=False,
@@ -533,8 +538,8 @@ def mecefo_preference_workspace_bytes(desc: PreferenceDesc) -> int:
 
 def mecefo_preference_loss(desc, logp, ref_logp, mask, offsets, loss, margins, rewards, dlogp, ws, stream=None):
     p, n = _ws(ws)
-    _check(lib().mecefo_preference_loss(C.byref(desc), _ptr(logp), _ptr(ref_logp), _ptr(mask), _ptr(offsets), _ptr(loss),
-                                        _ptr(margins), _ptr(rewards), _ptr(dlogp), p, n, _stream(stream)))
+    _check(lib().mecefo_preference_loss(C.byref(desc), _at(logp), _at(ref_logp), _at(mask), _at(offsets), _at(loss),
+                                        _at(margins), _at(rewards), _at(dlogp), p, n, _stream(stream)))
 
 
 def make_policy_desc(tokens, sequences, clip_low=0.2, clip_high=0.2, kl_coef=0.0, mean=MEAN_TOKENS, advantage_per_token=False,
@@ -550,8 +555,8 @@ def mecefo_policy_workspace_bytes(desc: PolicyDesc) -> int:
 
 def mecefo_policy_loss(desc, logp, old_logp, ref_logp, advantage, mask, offsets, loss, kl, clipped, dlogp, ws, stream=None):
     p, n = _ws(ws)
-    _check(lib().mecefo_policy_loss(C.byref(desc), _ptr(logp), _ptr(old_logp), _ptr(ref_logp), _ptr(advantage), _ptr(mask),
-                                    _ptr(offsets), _ptr(loss), _ptr(kl), _ptr(clipped), _ptr(dlogp), p, n, _stream(stream)))
+    _check(lib().mecefo_policy_loss(C.byref(desc), _at(logp), _at(old_logp), _at(ref_logp), _at(advantage), _at(mask),
+                                    _at(offsets), _at(loss), _at(kl), _at(clipped), _at(dlogp), p, n, _stream(stream)))
 
 
 STAGES = ["norm_fwd", "dgrad_down", "recompute", "swiglu_bwd", "dgrad_gate_up", "project", "contract",

@@ -362,10 +362,11 @@ mecefo_status_t norm_forward(const Ctx& c, const SideJob& j, hipStream_t s) {
 bool norm_rides(const Ctx& c) { return c.b * c.dm * c.esz <= (int64_t)4 << 20; }
 
 // dA = dY Wd  ->  recompute G, Z from U and apply the SwiGLU backward in the epilogue
-// (DG = dG, DZ = dZ, AA = A).   Sec. 3.3 (Rcomp).
+// (DG = dG, DZ = dZ, AA = A).   Sec. 3.3 (Rcomp).  G and Z given, as they are or as checkpoints: from those.
 mecefo_status_t recompute(const Ctx& c, const Bufs& bf, const void* U, int64_t ldu, const void* dY,
                                     int64_t lddy, const void* Wg, const void* Wu, const void* Wd,
-                                    const void* Gsaved, const void* Zsaved, int64_t ldgz, hipStream_t s, const SideJob* norm = nullptr) {
+                                    const void* Gsaved, const void* Zsaved, hipStream_t s, const SideJob* norm = nullptr,
+                                    const Ckpt* Gkept = nullptr, const Ckpt* Zkept = nullptr, bool as_riding = false) {
   const mecefo_ffn_desc_t& d = *c.d;
   char* base = bf.base;
   void* DG = base + bf.w.DG; void* DZ = base + bf.w.DZ; void* AA = base + bf.w.AA;
@@ -377,8 +378,9 @@ mecefo_status_t recompute(const Ctx& c, const Bufs& bf, const void* U, int64_t l
   GemmLaunch rec = new_launch(c, true, true, EPI_SWIGLU_BWD);   // G = U Wg^T, Z = U Wu^T, the SwiGLU backward in the epilogue
   rec.nprob = 1;
   rec.p[0] = prob(U, nullptr, ldu, Wg, Wu, d.ld_w_fd, DG, DZ, AA, c.ldf, b, c.ff, c.dm, 1, (int)c.ldf);
-  // a norm recompute that would ride on dA is a launch of its own then
-  const int pair = c.bf16 && !Gsaved ? gemm_bf16_pair_tile(down, rec, norm ? 3.2f : 0.f) : -1;
+  // a norm recompute that would ride on dA is a launch of its own then; as_riding: it has been one, and the launches are
+  // those of the call in which it rides, so that the sums are in the same order
+  const int pair = c.bf16 && !Gsaved && !Gkept ? gemm_bf16_pair_tile(down, rec, norm || as_riding ? 3.2f : 0.f) : -1;
   if (pair >= 0) {
     if (norm) TRY(norm_forward(c, *norm, s));
     STAGE(MECEFO_STAGE_RECOMPUTE, s);
@@ -393,9 +395,12 @@ mecefo_status_t recompute(const Ctx& c, const Bufs& bf, const void* U, int64_t l
     HIP_TRY(launch_gemm(down, s));
   }
   if (norm && !down.side_done) TRY(norm_forward(c, *norm, s));
-  if (Gsaved) {
+  if (Gkept) {
     STAGE(MECEFO_STAGE_SWIGLU_BWD, s);
-    HIP_TRY(launch_swiglu_bwd(c.bf16, Gsaved, Zsaved, ldgz, DG, DZ, AA, c.ldf, c.b, c.ff, (int)c.ldf, s));
+    HIP_TRY(launch_swiglu_bwd_ckpt(c.bf16, *Gkept, *Zkept, DG, DZ, AA, c.ldf, c.b, c.ff, s));
+  } else if (Gsaved) {
+    STAGE(MECEFO_STAGE_SWIGLU_BWD, s);
+    HIP_TRY(launch_swiglu_bwd(c.bf16, Gsaved, Zsaved, d.ld_act_f, DG, DZ, AA, c.ldf, c.b, c.ff, (int)c.ldf, s));
   } else {
     STAGE(MECEFO_STAGE_RECOMPUTE, s);
     rec.clk = g_prof.cur_clk;
@@ -701,10 +706,12 @@ FwdWs fwd_layout(const Ctx& c, const mecefo_attn_desc_t& a) {
 }
 
 // The block forward behind mecefo_block_fwd.  plan: the layout that every layer of one public call shares, NULL to
-// make it here; tables_ready: the workspace holds the rotary tables of a previous layer of the same plan.
+// make it here; tables_ready: the workspace holds the rotary tables of a previous layer of the same plan; ckpt: where H
+// goes as an 8-bit checkpoint besides.
 mecefo_status_t block_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn,
                           const mecefo_block_fwd_inputs_t* in, const mecefo_block_fwd_outputs_t* out,
-                          const FwdWs* plan, void* ws, size_t ws_bytes, void* hip_stream, bool tables_ready);
+                          const FwdWs* plan, void* ws, size_t ws_bytes, void* hip_stream, bool tables_ready,
+                          const Ckpt* ckpt = nullptr);
 
 mecefo_status_t check_lowrank_args(const Ctx& c, const mecefo_proj_t P[3], mecefo_side_t side, int exact_mask = 0) {
   if (side != MECEFO_SIDE_INPUT && side != MECEFO_SIDE_OUTPUT) return fail(MECEFO_ERR_INVALID_ARG, "side must be MECEFO_SIDE_INPUT or MECEFO_SIDE_OUTPUT");
@@ -717,10 +724,8 @@ mecefo_status_t check_lowrank_args(const Ctx& c, const mecefo_proj_t P[3], mecef
 
 // ---- neighbor-mode backward ------------------------------------------------------------------
 struct KeptCkpts { const mecefo_ckpt_t *H, *G, *Z; };
-// Room behind the workspace of the backward for the unpacked H, G and Z.
-size_t kept_bytes(const Ctx& c) {
-  return (size_t)(up(c.b * c.dm * c.esz, 256) + 2 * up(c.b * c.ldf * c.esz, 256)) + 256;
-}
+// Room behind the workspace of the backward for the values of H.
+size_t kept_bytes(const Ctx& c) { return (size_t)up(c.b * c.dm * c.esz, 256); }
 
 // The neighbor-mode backward behind its entry points.  kept: the stored tensors as 8-bit checkpoints, which are unpacked
 // into the workspace (H, opt->G and opt->Z are then NULL), or NULL.
@@ -762,33 +767,28 @@ mecefo_status_t block_bwd_skip(const mecefo_ffn_desc_t* desc, const void* H, con
   TRY(carve(c, r, side, ws, ws_bytes, &bf, kept ? kept_bytes(c) : 0));
   hipStream_t s = (hipStream_t)hip_stream;
   char* base = bf.base;
-  int64_t ldh = desc->ld_act_d, ldgz = desc->ld_act_f;
-  if (kept && c.b > 0) {
-    char* at = base + bf.w.total;      // the layout's slack of 256 bytes lies in front
-    auto unpacked = [&](const Ckpt& k, int cols, int64_t ld) -> const void* {
-      void* X = at;
-      at += up(c.b * ld * c.esz, 256);
-      return launch_ckpt_unpack(c.bf16, k, c.b, cols, X, ld, s) == hipSuccess ? X : nullptr;
-    };
+  int64_t ldh = desc->ld_act_d;
+  const bool unpack = kept && c.b > 0;
+  if (unpack) {
+    void* Hk = base + bf.w.total;      // the layout's slack of 256 bytes lies in front
     STAGE(MECEFO_STAGE_NORM_FWD, s);
+    if (gamma) HIP_TRY(launch_rmsnorm_ckpt(c.bf16, kh, gamma, desc->rms_eps, Hk, base + bf.w.U, (float*)(base + bf.w.rstd), c.b, c.dm, s));
+    else HIP_TRY(launch_ckpt_unpack(c.bf16, kh, c.b, c.dm, Hk, c.dm, s));
+    H = Hk;
     ldh = c.dm;
-    ldgz = c.ldf;
-    H = unpacked(kh, c.dm, ldh);
-    if (kept->G) { Gs = unpacked(kg, c.ff, ldgz); Zs = unpacked(kz, c.ff, ldgz); }
-    if (!H || (kept->G && (!Gs || !Zs))) return fail(MECEFO_ERR_LAUNCH, "unpacking a checkpoint: %s", hipGetErrorString(hipGetLastError()));
   }
   const void* U = H;
   int64_t ldu = ldh;
   const SideJob norm = norm_job(c, H, ldh, gamma, base + bf.w.U, (float*)(base + bf.w.rstd));
-  const bool rides = gamma && c.b > 0 && norm_rides(c);
+  const bool small = gamma && c.b > 0 && norm_rides(c), rides = small && !unpack;
   if (gamma && c.b > 0) {  // recompute the norm output from the stored tensor
-    if (!rides) TRY(norm_forward(c, norm, s));
+    if (!rides && !unpack) TRY(norm_forward(c, norm, s));
     U = base + bf.w.U;
     ldu = c.dm;
   }
   void* dUb = base + bf.w.dU;
   const LowRank q = low_rank(c, bf, U, ldu, dOut, desc->ld_act_d, P, side, exact_mask);
-  TRY(recompute(c, bf, U, ldu, dOut, desc->ld_act_d, Wg, Wu, Wd, Gs, Zs, ldgz, s, rides ? &norm : nullptr));
+  TRY(recompute(c, bf, U, ldu, dOut, desc->ld_act_d, Wg, Wu, Wd, Gs, Zs, s, rides ? &norm : nullptr, kg.q ? &kg : nullptr, &kz, small));
   // Eq. (2) reads dOut (the down projection's output gradient) and, without a norm, H itself: when dX
   // is a buffer of its own the norm backward goes first, while dU is still in the caches; when dX overwrites dOut (or H)
   // it has to wait for the contraction, which needs the partial buffer.  The expand launch carries the sum of the gain
@@ -993,7 +993,7 @@ mecefo_status_t mecefo_ffn_bwd_exact(const mecefo_ffn_desc_t* desc, const void* 
   Bufs bf;
   TRY(carve(c, r0, MECEFO_SIDE_INPUT, ws, ws_bytes, &bf));
   hipStream_t s = (hipStream_t)hip_stream;
-  TRY(recompute(c, bf, U, desc->ld_act_d, dY, desc->ld_act_d, Wg, Wu, Wd, G, Z, desc->ld_act_f, s));
+  TRY(recompute(c, bf, U, desc->ld_act_d, dY, desc->ld_act_d, Wg, Wu, Wd, G, Z, s));
   TRY(dgrad(c, bf, Wg, Wu, dU, desc->ld_act_d, s));
   // exact Wgrad: dWg = dG^T U, dWu = dZ^T U [f x d]; dWd = dY^T A [d x f]; contraction over tokens
   STAGE(MECEFO_STAGE_WGRAD_EXACT, s);
@@ -1028,7 +1028,7 @@ mecefo_status_t mecefo_ffn_bwd_lowrank(const mecefo_ffn_desc_t* desc, const void
   TRY(carve(c, r, side, ws, ws_bytes, &bf));
   hipStream_t s = (hipStream_t)hip_stream;
   const LowRank q = low_rank(c, bf, U, desc->ld_act_d, dY, desc->ld_act_d, P, side, 0);
-  TRY(recompute(c, bf, U, desc->ld_act_d, dY, desc->ld_act_d, Wg, Wu, Wd, nullptr, nullptr, 0, s));
+  TRY(recompute(c, bf, U, desc->ld_act_d, dY, desc->ld_act_d, Wg, Wu, Wd, nullptr, nullptr, s));
   TRY(dgrad_and_project(c, bf, q, Wg, Wu, dU, desc->ld_act_d, s));
   void* dW[3] = {dWg, dWu, dWd};
   TRY(wgrad_contract(c, bf, q, dW, accumulate, s));
@@ -1136,7 +1136,7 @@ mecefo_status_t mecefo_block_bwd_full(const mecefo_ffn_desc_t* desc, const mecef
   const SideJob norm = norm_job(c, in->H, d.ld_act_d, in->g_ffn, Ub, rstd);
   const bool rides = any && norm_rides(c);
   if (any && !rides) TRY(norm_forward(c, norm, s));
-  TRY(recompute(c, bf, Ub, dm, in->dOut, d.ld_act_d, in->Wg, in->Wu, in->Wd, nullptr, nullptr, 0, s, rides ? &norm : nullptr));
+  TRY(recompute(c, bf, Ub, dm, in->dOut, d.ld_act_d, in->Wg, in->Wu, in->Wd, nullptr, nullptr, s, rides ? &norm : nullptr));
   Parts parts;
   auto ffn_norm = [&]() {
     return norm_bwd_args(c, bf, fw, parts, in->H, d.ld_act_d, in->g_ffn, in->dOut, d.ld_act_d, dH, dm, true);
@@ -1313,7 +1313,8 @@ mecefo_status_t mecefo_block_fwd(const mecefo_ffn_desc_t* desc, const mecefo_att
 namespace {
 mecefo_status_t block_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn,
                           const mecefo_block_fwd_inputs_t* in, const mecefo_block_fwd_outputs_t* out,
-                          const FwdWs* plan, void* ws, size_t ws_bytes, void* hip_stream, bool tables_ready) {
+                          const FwdWs* plan, void* ws, size_t ws_bytes, void* hip_stream, bool tables_ready,
+                          const Ckpt* ckpt) {
   Ctx c;
   TRY(check_desc(desc, &c));
   TRY(check_attn(c, attn));
@@ -1406,7 +1407,8 @@ mecefo_status_t block_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_
     HIP_TRY(launch_gemm(g, s));
   }
   // FFN: U = norm(H), A = silu(U Wg^T) * (U Wu^T), Out = H + A Wd^T
-  HIP_TRY(launch_rmsnorm_fwd(c.bf16, out->H, d.ld_act_d, in->g_ffn, d.rms_eps, Xn, dm, rstd, c.b, dm, s));
+  if (ckpt) HIP_TRY(launch_rmsnorm_pack(c.bf16, out->H, d.ld_act_d, in->g_ffn, d.rms_eps, Xn, rstd, c.b, dm, *ckpt, s));
+  else HIP_TRY(launch_rmsnorm_fwd(c.bf16, out->H, d.ld_act_d, in->g_ffn, d.rms_eps, Xn, dm, rstd, c.b, dm, s));
   void* AA = base + w.A;
   {
     GemmLaunch g = new_launch(c, true, true, EPI_SWIGLU_FWD);
@@ -1458,13 +1460,10 @@ mecefo_status_t stack_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_
     void* y = l == n_layers - 1 ? X_out : pp[l & 1];
     mecefo_block_fwd_outputs_t out = {y, kept ? base + 2 * act : H[l], nullptr, nullptr, nullptr, nullptr, nullptr};
     // every layer of the call uses the same workspace and layout: the angle tables of the first one serve them all
-    mecefo_status_t st = block_fwd(desc, attn, &in, &out, &plan, inner_ws, ws_bytes - front, hip_stream, l > 0);
+    Ckpt k;
+    if (kept) TRY((mecefo_status_t)check_ckpt(&kept[l], c.b, c.dm, "H", &k));
+    mecefo_status_t st = block_fwd(desc, attn, &in, &out, &plan, inner_ws, ws_bytes - front, hip_stream, l > 0, kept ? &k : nullptr);
     if (st != MECEFO_OK) return st;
-    if (kept && c.b > 0) {
-      Ckpt k;
-      TRY((mecefo_status_t)check_ckpt(&kept[l], c.b, c.dm, "H", &k));
-      HIP_TRY(launch_ckpt_pack(c.bf16, out.H, desc->ld_act_d, c.b, c.dm, k, (hipStream_t)hip_stream));
-    }
     x = y;
   }
   return MECEFO_OK;

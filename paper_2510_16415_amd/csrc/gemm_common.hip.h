@@ -351,6 +351,13 @@ template <bool PRECISE> __device__ inline float sigmoid_f(float g) {
   }
 }
 
+// SwiGLU backward of one element: dA and the pre-activations to dG, dZ and A.
+struct SwigluGrad { float dg, dz, a; };
+template <bool PRECISE> __device__ inline SwigluGrad swiglu_grad(float g, float z, float da) {
+  const float sg = sigmoid_f<PRECISE>(g), s = g * sg;
+  return SwigluGrad{da * z * (sg * (1.0f + g * (1.0f - sg))), da * s, s * z};
+}
+
 template <int EPI> constexpr bool kUnhandledEpilogue = false;
 
 // EPI_HEAD_GRAD: what a row's gradients are made of; c = 0 where the row has no label among the columns.

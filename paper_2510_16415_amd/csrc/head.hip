@@ -15,72 +15,94 @@ namespace {
 
 __device__ inline bool counted(int64_t label, int vocab) { return label >= 0 && label < vocab; }
 
-// lse and logp of a row of fp32 products z (before logit_scale), a workgroup per row.
-__global__ __launch_bounds__(256) void head_rows_kernel(const float* __restrict__ Z, int64_t ldz, int vocab, float scale,
+// lse and logp of a row of fp32 products z (before logit_scale), a workgroup per row, in one pass with a running maximum.
+__global__ __launch_bounds__(1024) void head_rows_kernel(const float* __restrict__ Z, int64_t ldz, int vocab, float scale,
                                                         const int64_t* __restrict__ labels, float* __restrict__ logp,
                                                         float* __restrict__ lse) {
-  __shared__ float red[4];
+  __shared__ float2 red[16];
   const int64_t row = blockIdx.x;
   const float* z = Z + row * ldz;
-  float m = -INFINITY;
-  for (int v = threadIdx.x; v < vocab; v += 256) m = fmaxf(m, z[v] * scale);
+  auto join = [](float2 x, float2 y) {      // a share without columns is (-inf, 0)
+    const float m = fmaxf(x.x, y.x), k = m == -INFINITY ? 0.f : m;
+    return float2{m, x.y * expf(x.x - k) + y.y * expf(y.x - k)};
+  };
+  float2 a = {-INFINITY, 0.f};
+  for (int v0 = 4 * threadIdx.x; v0 < vocab; v0 += 4096) {      // rows are whole vectors of eight
+    typedef __attribute__((ext_vector_type(4))) float f4;
+    const f4 x = *(const f4*)(z + v0);
+    float y[4], m = a.x;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  __syncthreads();
-  float s = 0.f;
-  for (int v = threadIdx.x; v < vocab; v += 256) s += expf(z[v] * scale - m);
+    for (int e = 0; e < 4; ++e) {
+      y[e] = v0 + e < vocab ? x[e] * scale : -INFINITY;
+      m = fmaxf(m, y[e]);
+    }
+    float s = a.x == -INFINITY ? 0.f : a.y * expf(a.x - m);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    for (int e = 0; e < 4; ++e) s += expf(y[e] - m);
+    a = float2{m, s};
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) a = join(a, float2{__shfl_xor(a.x, o, 64), __shfl_xor(a.y, o, 64)});
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
   __syncthreads();
   if (threadIdx.x != 0) return;
-  const float l = m + logf((red[0] + red[1]) + (red[2] + red[3]));
+  for (int w = 1; w < 16; ++w) a = join(a, red[w]);
+  const float l = a.x + logf(a.y);
   const int64_t label = labels[row];
   logp[row] = counted(label, vocab) ? z[label] * scale - l : 0.f;
   if (lse) lse[row] = l;
 }
 
 // lse and logp from the parts that the products' epilogue leaves: (largest z, sum of exp(z - that)) of a row over part_cols
-// columns, [parts][rows], and z at the label.  16 rows to a workgroup, 64 threads share out a row's parts.
+// columns, [parts][rows], and z at the label.  ROWS neighbouring rows to a workgroup, 1024 / ROWS threads share out a row's
+// parts: 16 rows read whole lines, where there are few rows 2 use more of the chip (77 rows of 500 parts: HEAD_PARTS us).
+template <int ROWS>
 __global__ __launch_bounds__(1024) void head_parts_kernel(const float2* __restrict__ part, int parts, int rows, int vocab,
                                                           const float* __restrict__ zl, const int64_t* __restrict__ labels,
                                                           float* __restrict__ logp, float* __restrict__ lse) {
-  __shared__ float2 red[64][16];
-  const int r = threadIdx.x & 15, g = threadIdx.x >> 4, row = blockIdx.x * 16 + r;
-  float2 a = {-INFINITY, 0.f};
-  auto join = [](float2 x, float2 y) {      // a part without columns is (-inf, 0)
-    const float m = fmaxf(x.x, y.x);
-    return m == -INFINITY ? float2{m, x.y + y.y} : float2{m, x.y * expf(x.x - m) + y.y * expf(y.x - m)};
+  constexpr int G = 1024 / ROWS;
+  __shared__ float2 red[16][ROWS];
+  const int r = threadIdx.x % ROWS, g = threadIdx.x / ROWS, row = blockIdx.x * ROWS + r;
+  auto join = [](float2 x, float2 y) {      // a share without parts is (-inf, 0)
+    const float m = fmaxf(x.x, y.x), k = m == -INFINITY ? 0.f : m;
+    return float2{m, x.y * __builtin_amdgcn_exp2f(1.44269504088896341f * (x.x - k)) + y.y * __builtin_amdgcn_exp2f(1.44269504088896341f * (y.x - k))};
   };
-  if (row < rows) {
+  float2 a = {-INFINITY, 0.f};
+  const int at = row < rows ? row : rows - 1;
 #pragma unroll 4
-    for (int k = g; k < parts; k += 64) a = join(a, part[(int64_t)k * rows + row]);
-  }
-  red[g][r] = a;
+  for (int k = g; k < parts; k += G) a = join(a, part[(int64_t)k * rows + at]);
+#pragma unroll
+  for (int o = ROWS; o < 64; o *= 2) a = join(a, float2{__shfl_xor(a.x, o, 64), __shfl_xor(a.y, o, 64)});
+  if ((threadIdx.x & 63) < ROWS) red[threadIdx.x >> 6][r] = a;
   __syncthreads();
-  for (int n = 32; n > 0; n >>= 1) {
-    if (g < n) red[g][r] = join(red[g][r], red[g + n][r]);
-    __syncthreads();
-  }
-  if (g != 0 || row >= rows) return;
-  const float l = red[0][r].x + logf(red[0][r].y);
+  if (threadIdx.x >= ROWS || row >= rows) return;
+#pragma unroll
+  for (int w = 1; w < 16; ++w) a = join(a, red[w][r]);
+  const float l = a.x + logf(a.y);
   logp[row] = counted(labels[row], vocab) ? zl[row] - l : 0.f;
   if (lse) lse[row] = l;
 }
 
-// out[row, 0 .. cols) = sum of the parts [k][row, col], in their order.
-template <typename T>
+// out[row, 0 .. cols) = sum of the parts [k][row, col], in their order, V columns per thread.
+template <typename T, int V>
 __global__ __launch_bounds__(256) void head_sum_kernel(const float* __restrict__ part, int parts, int64_t rows, int cols,
                                                        T* __restrict__ out, int64_t ldo) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  struct alignas(4 * V) In { float e[V]; };
+  struct alignas(sizeof(T) * V) Out { T e[V]; };
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
   if (i >= rows * cols) return;
   const int64_t row = i / cols;
-  float s = part[i];
-  for (int k = 1; k < parts; ++k) s += part[(int64_t)k * rows * cols + i];
-  out[row * ldo + (i - row * cols)] = (T)s;
+  In s = *(const In*)(part + i);
+#pragma unroll 4
+  for (int k = 1; k < parts; ++k) {
+    const In x = *(const In*)(part + (int64_t)k * rows * cols + i);
+#pragma unroll
+    for (int e = 0; e < V; ++e) s.e[e] += x.e[e];
+  }
+  Out o;
+#pragma unroll
+  for (int e = 0; e < V; ++e) o.e[e] = (T)s.e[e];
+  *(Out*)(out + row * ldo + (i - row * cols)) = o;
 }
 
 __global__ __launch_bounds__(256) void head_zero_kernel(uint32_t* p, int n) {
@@ -247,11 +269,14 @@ mecefo_status_t mecefo_head_logprob_fwd(const mecefo_head_desc_t* desc, const vo
     g.p[0].scale = desc->logit_scale;
   }
   HIP_TRY(launch_gemm(g, s));
-  if (h.bf16)
-    hipLaunchKernelGGL(head_parts_kernel, dim3((h.b + 15) / 16), dim3(1024), 0, s, (const float2*)(base + w.Z), cdiv(h.vocab, g.part_cols),
-                       h.b, h.vocab, (const float*)(base + w.zl), labels, logp, lse);
-  else
-    hipLaunchKernelGGL(head_rows_kernel, dim3(h.b), dim3(256), 0, s, (const float*)(base + w.Z), h.ldz, h.vocab, desc->logit_scale, labels,
+  if (h.bf16) {
+    const float2* part = (const float2*)(base + w.Z);
+    const float* zl = (const float*)(base + w.zl);
+    const int parts = cdiv(h.vocab, g.part_cols);
+    if (h.b >= 2 * kCUs) hipLaunchKernelGGL(head_parts_kernel<16>, dim3(cdiv(h.b, 16)), dim3(1024), 0, s, part, parts, h.b, h.vocab, zl, labels, logp, lse);
+    else hipLaunchKernelGGL(head_parts_kernel<2>, dim3(cdiv(h.b, 2)), dim3(1024), 0, s, part, parts, h.b, h.vocab, zl, labels, logp, lse);
+  } else
+    hipLaunchKernelGGL(head_rows_kernel, dim3(h.b), dim3(1024), 0, s, (const float*)(base + w.Z), h.ldz, h.vocab, desc->logit_scale, labels,
                        logp, lse);
   HIP_TRY(hipGetLastError());
   return MECEFO_OK;
@@ -310,9 +335,15 @@ mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const vo
     HIP_TRY(launch_gemm(g, s));
     if (parts > 1) {
       const float* part = (const float*)(base + w.part);
-      const unsigned grid = (unsigned)(((int64_t)h.b * h.dm + 255) / 256);
-      if (h.bf16) hipLaunchKernelGGL(head_sum_kernel<__bf16>, dim3(grid), dim3(256), 0, s, part, parts, (int64_t)h.b, h.dm, (__bf16*)dU, lddu);
-      else hipLaunchKernelGGL(head_sum_kernel<float>, dim3(grid), dim3(256), 0, s, part, parts, (int64_t)h.b, h.dm, (float*)dU, lddu);
+      const int64_t n = (int64_t)h.b * h.dm;
+      auto sum = [&](auto type, auto v) {      // bf16 rows are whole vectors of eight
+        using T = decltype(type);
+        constexpr int V = decltype(v)::value;
+        hipLaunchKernelGGL((head_sum_kernel<T, V>), dim3((unsigned)((n / V + 255) / 256)), dim3(256), 0, s, part, parts, (int64_t)h.b, h.dm, (T*)dU, lddu);
+      };
+      if (h.bf16) sum(__bf16{}, std::integral_constant<int, 4>{});
+      else if (h.dm % 4 == 0 && lddu % 4 == 0 && (uintptr_t)dU % 16 == 0) sum(float{}, std::integral_constant<int, 4>{});
+      else sum(float{}, std::integral_constant<int, 1>{});
       HIP_TRY(hipGetLastError());
     }
     if (gamma) {  // dX = normbwd(dU): the norm backward adds a residual gradient, here a row of zeros with stride 0

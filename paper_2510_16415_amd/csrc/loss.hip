@@ -2,34 +2,41 @@
 // log ratios and the clipped policy loss with a KL term.  Tokens lie packed one sequence behind the other; `offsets` says where
 // each begins, and a mask which tokens count.  A few bytes per token: the launches and the latency of the loads are what they
 // take, so every sequence is cut into slices, a workgroup each, in two launches: one takes the sums that the gradient of a
-// token depends on (its sequence's ratio, the number of counted tokens), the other the tokens' gradients.  Sums are held in 64
+// token depends on (its sequence's ratio, the number of counted tokens), the other the tokens' gradients.  A small batch is one
+// workgroup's, and one launch's.  Sums are held in 64
 // bits, each added up in an order that only the sizes decide.
 #include <math.h>
 
 #include "../../include/mecefo.h"
+#include "loss_ranges.h"
 #include "mecefo_internal.h"
 
 namespace mecefo {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSliceTokens = 2048;   // tokens of a slice, in a sequence of mean length
+constexpr int kSliceTokens = 1024;   // tokens of a slice, in a sequence of mean length
 constexpr int kMaxSlices = 64;
+constexpr int kWaveSlices = 16;
+constexpr int kSmallTokens = 4096, kSmallSeqs = 512;
 
 struct Part { double sum; double count; };
 
-struct Range { int64_t lo, hi; };
-// Slice `j` of `n` of sequence `k`; offsets outside [0, tokens], or that decrease, give ranges inside it.
-__device__ inline Range sequence(const int64_t* offsets, int64_t tokens, int k) {
-  const int64_t a = offsets[k], b = offsets[k + 1];
-  Range r;
-  r.lo = a < 0 ? 0 : (a > tokens ? tokens : a);
-  r.hi = b < r.lo ? r.lo : (b > tokens ? tokens : b);
-  return r;
-}
-__device__ inline Range slice(Range r, int j, int n) {
-  const int64_t len = r.hi - r.lo;
-  return Range{r.lo + len * j / n, r.lo + len * (j + 1) / n};
+__device__ inline TokenRange sequence(const int64_t* offsets, int64_t tokens, int k) { return token_range(offsets[k], offsets[k + 1], tokens); }
+
+// Calls f(token, loaded values) for the tokens t0, t0 + stride, ... of a range, kAhead of them loaded before the first is used:
+// a few bytes a token, so the time is that of the loads' latency.
+constexpr int kAhead = 4;
+template <class Load, class Use>
+__device__ inline void for_tokens(TokenRange r, int first, int stride, Load load, Use use) {
+  for (int64_t t = r.lo + first; t < r.hi; t += (int64_t)kAhead * stride) {
+    decltype(load(t)) v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) v[u] = load(t + (int64_t)u * stride < r.hi ? t + (int64_t)u * stride : t);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (t + (int64_t)u * stride < r.hi) use(t + (int64_t)u * stride, v[u]);
+  }
 }
 
 __device__ inline double wave_sum(double v) {
@@ -37,20 +44,27 @@ __device__ inline double wave_sum(double v) {
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   return v;
 }
-// The sum over the workgroup, in every thread.
-__device__ inline double block_sum(double v, double* red) {
-  v = wave_sum(v);
+// Sums over the workgroup, in every thread.
+template <int N>
+__device__ inline void block_sums(double (&v)[N]) {
+  __shared__ double red[16][N];
+#pragma unroll
+  for (int q = 0; q < N; ++q) v[q] = wave_sum(v[q]);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  if ((threadIdx.x & 63) == 0)
+    for (int q = 0; q < N; ++q) red[threadIdx.x >> 6][q] = v[q];
   __syncthreads();
-  double s = red[0];
-  for (int w = 1; w < (int)(blockDim.x >> 6); ++w) s += red[w];
-  return s;
+#pragma unroll
+  for (int q = 0; q < N; ++q) {
+    v[q] = red[0][q];
+    for (int w = 1; w < (int)(blockDim.x >> 6); ++w) v[q] += red[w][q];
+  }
 }
-
-// log(1 + exp(t)) without overflow; sigmoid.
-__device__ inline double softplus(double t) { return (t > 0 ? t : 0.0) + log1p(exp(-fabs(t))); }
-__device__ inline double sigmoid(double t) { return 1.0 / (1.0 + exp(-t)); }
+__device__ inline double block_sum(double x) {
+  double v[1] = {x};
+  block_sums(v);
+  return v[0];
+}
 
 struct PrefArgs {
   const float *logp, *ref;
@@ -63,36 +77,56 @@ struct PrefArgs {
   double beta, smooth, margin, grad_scale;
 };
 
+// The slices of one sequence added up, by one wave (slices <= 64), in all its lanes.
 __device__ inline Part add_slices(const Part* p, int n) {
+  const int lane = threadIdx.x & 63;
+  const Part x = lane < n ? p[lane] : Part{0.0, 0.0};
+  return Part{wave_sum(x.sum), wave_sum(x.count)};
+}
+// Sum over a range of the counted tokens' log ratios, and how many there are, a thread's share.
+struct Ratio { float logp, ref; uint8_t on; };
+__device__ inline Part ratio_sum(const PrefArgs& a, TokenRange r, int first, int stride) {
   Part s = {0.0, 0.0};
-  for (int j = 0; j < n; ++j) { s.sum += p[j].sum; s.count += p[j].count; }
+  for_tokens(r, first, stride,
+             [&](int64_t t) { return Ratio{a.logp[t], a.ref ? a.ref[t] : 0.f, a.mask ? a.mask[t] : (uint8_t)1}; },
+             [&](int64_t, const Ratio& x) {
+               s.sum += x.on ? (double)x.logp - (double)x.ref : 0.0;
+               s.count += x.on ? 1.0 : 0.0;
+             });
   return s;
 }
-// Sum over a slice of the counted tokens' log ratios, and how many there are.
-__device__ inline Part ratio_sum(const PrefArgs& a, Range r) {
-  Part s = {0.0, 0.0};
-  for (int64_t t = r.lo + threadIdx.x; t < r.hi; t += blockDim.x) {
-    const bool on = !a.mask || a.mask[t];
-    const double x = (double)a.logp[t] - (a.ref ? (double)a.ref[t] : 0.0);
-    s.sum += on ? x : 0.0;
-    s.count += on ? 1.0 : 0.0;
-  }
-  return s;
+// The gradients of a range: g(), which may take a while, is asked for once the first tokens' masks are on their way.
+template <class G>
+__device__ inline void write_gradients(const PrefArgs& a, TokenRange r, int first, int stride, G g) {
+  const int64_t t0 = r.lo + first;
+  uint8_t on[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) on[u] = a.mask && t0 + (int64_t)u * stride < r.hi ? a.mask[t0 + (int64_t)u * stride] : (uint8_t)1;
+  const float v = g();
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u)
+    if (t0 + (int64_t)u * stride < r.hi) a.dlogp[t0 + (int64_t)u * stride] = on[u] ? v : 0.f;
+  for_tokens(r, first + kAhead * stride, stride, [&](int64_t t) { return a.mask ? a.mask[t] : (uint8_t)1; },
+             [&](int64_t t, uint8_t m) { a.dlogp[t] = m ? v : 0.f; });
 }
 // beta times the sum, or the mean, of the ratios of one sequence, and what one of its tokens contributes to that.
 __device__ inline double reward(const PrefArgs& a, Part p, double* per_token) {
   *per_token = a.mean ? a.beta / (p.count > 1.0 ? p.count : 1.0) : a.beta;
   return p.sum * *per_token;
 }
-__device__ inline double pair_loss(const PrefArgs& a, double h) { return (1.0 - a.smooth) * softplus(-h) + a.smooth * softplus(h); }
-__device__ inline double pair_slope(const PrefArgs& a, double h) { return a.smooth * sigmoid(h) - (1.0 - a.smooth) * sigmoid(-h); }
+// A pair's loss and its slope in h, from one exponential: softplus(t) = max(t, 0) + log1p(exp(-|t|)).
+struct PairLoss { double loss, slope; };
+__device__ inline PairLoss pair_loss(const PrefArgs& a, double h) {
+  const double e = exp(-fabs(h)), l = log1p(e), s = 1.0 / (1.0 + e), up = h >= 0 ? s : e * s, down = h >= 0 ? e * s : s;
+  return PairLoss{(1.0 - a.smooth) * ((h < 0 ? -h : 0.0) + l) + a.smooth * ((h > 0 ? h : 0.0) + l), a.smooth * up - (1.0 - a.smooth) * down};
+}
 
 __global__ __launch_bounds__(kThreads) void preference_sums_kernel(const PrefArgs a) {
-  __shared__ double red[kThreads / 64];
   const int k = blockIdx.x / a.slices, j = blockIdx.x - k * a.slices;
-  const Part p = ratio_sum(a, slice(sequence(a.offsets, a.tokens, k), j, a.slices));
-  const double sum = block_sum(p.sum, red), count = block_sum(p.count, red);
-  if (threadIdx.x == 0) a.parts[blockIdx.x] = Part{sum, count};
+  const Part p = ratio_sum(a, token_slice(sequence(a.offsets, a.tokens, k), j, a.slices), threadIdx.x, kThreads);
+  double v[2] = {p.sum, p.count};
+  block_sums(v);
+  if (threadIdx.x == 0) a.parts[blockIdx.x] = Part{v[0], v[1]};
 }
 
 // Zeros for the tokens in front of the first sequence and behind the last one.
@@ -103,64 +137,96 @@ __device__ inline void clear_outside(const int64_t* offsets, int64_t tokens, int
 }
 
 // Workgroups 0 .. 2 * pairs * slices - 1: the gradients of a slice; the one behind them: the mean loss, every pair's margin and
-// rewards, and the tokens of no sequence.
+// rewards, and the tokens of no sequence.  It takes a wave to a pair where sequences have many slices, else a thread (64 pairs
+// of 4 slices: the launch 28 us with a wave to a pair, 6 with a thread).
 __global__ __launch_bounds__(kThreads) void preference_grad_kernel(const PrefArgs a) {
-  __shared__ double red[kThreads / 64];
   const int grads = 2 * a.pairs * a.slices;
   if ((int)blockIdx.x == grads) {
     double total = 0.0;
-    for (int i = threadIdx.x; i < a.pairs; i += kThreads) {
+    auto pair = [&](int i, const Part& chosen, const Part& other) {
       double w;
-      const double rc = reward(a, add_slices(a.parts + (int64_t)(2 * i) * a.slices, a.slices), &w);
-      const double rr = reward(a, add_slices(a.parts + (int64_t)(2 * i + 1) * a.slices, a.slices), &w);
-      const double h = rc - rr - a.margin;
-      total += pair_loss(a, h);
+      const double rc = reward(a, chosen, &w), rr = reward(a, other, &w), h = rc - rr - a.margin;
+      total += pair_loss(a, h).loss;
       if (a.margins) a.margins[i] = (float)h;
       if (a.rewards) { a.rewards[2 * i] = (float)rc; a.rewards[2 * i + 1] = (float)rr; }
+    };
+    if (a.slices >= kWaveSlices) {
+      for (int i = threadIdx.x >> 6; i < a.pairs; i += kThreads / 64) {
+        const Part c = add_slices(a.parts + (int64_t)(2 * i) * a.slices, a.slices), o = add_slices(a.parts + (int64_t)(2 * i + 1) * a.slices, a.slices);
+        if ((threadIdx.x & 63) == 0) pair(i, c, o);
+      }
+    } else {
+      for (int i = threadIdx.x; i < a.pairs; i += kThreads) {
+        Part p[2] = {{0.0, 0.0}, {0.0, 0.0}};
+        for (int k = 0; k < 2; ++k)
+#pragma unroll 4
+          for (int j = 0; j < a.slices; ++j) {
+            const Part x = a.parts[(int64_t)(2 * i + k) * a.slices + j];
+            p[k].sum += x.sum; p[k].count += x.count;
+          }
+        pair(i, p[0], p[1]);
+      }
     }
-    total = block_sum(total, red);
+    total = block_sum(total);
     if (threadIdx.x == 0) a.loss[0] = a.pairs > 0 ? (float)(total / a.pairs) : 0.f;
     clear_outside(a.offsets, a.tokens, 2 * a.pairs, a.dlogp);
     return;
   }
   const int k = blockIdx.x / a.slices, j = blockIdx.x - k * a.slices;
-  double wc, wr;
-  const int c = k & ~1;
-  const double rc = reward(a, add_slices(a.parts + (int64_t)c * a.slices, a.slices), &wc);
-  const double rr = reward(a, add_slices(a.parts + (int64_t)(c + 1) * a.slices, a.slices), &wr);
-  const double slope = pair_slope(a, rc - rr - a.margin) * a.grad_scale / a.pairs;
-  const float g = (float)(k & 1 ? -slope * wr : slope * wc);
-  const Range r = slice(sequence(a.offsets, a.tokens, k), j, a.slices);
-  for (int64_t t = r.lo + threadIdx.x; t < r.hi; t += kThreads) a.dlogp[t] = !a.mask || a.mask[t] ? g : 0.f;
+  const TokenRange r = token_slice(sequence(a.offsets, a.tokens, k), j, a.slices);
+  write_gradients(a, r, threadIdx.x, kThreads, [&]() {
+    double wc, wr;
+    const int c = k & ~1;
+    const Part pc = add_slices(a.parts + (int64_t)c * a.slices, a.slices), pr = add_slices(a.parts + (int64_t)(c + 1) * a.slices, a.slices);
+    const double rc = reward(a, pc, &wc), rr = reward(a, pr, &wr);
+    const double g = pair_loss(a, rc - rr - a.margin).slope * a.grad_scale / a.pairs;
+    return (float)(k & 1 ? -g * wr : g * wc);
+  });
 }
+
+// A small batch in one workgroup and one launch: a wave to a sequence, the sums in LDS.
+__global__ __launch_bounds__(1024) void preference_small_kernel(const PrefArgs a) {
+  __shared__ Part parts[kSmallSeqs];
+  __shared__ float slope[kSmallSeqs];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  for (int k = wave; k < 2 * a.pairs; k += 16) {
+    const Part p = ratio_sum(a, sequence(a.offsets, a.tokens, k), lane, 64);
+    const double sum = wave_sum(p.sum), count = wave_sum(p.count);
+    if (lane == 0) parts[k] = Part{sum, count};
+  }
+  __syncthreads();
+  double total = 0.0;
+  for (int i = threadIdx.x; i < a.pairs; i += 1024) {
+    double wc, wr;
+    const double rc = reward(a, parts[2 * i], &wc), rr = reward(a, parts[2 * i + 1], &wr), h = rc - rr - a.margin;
+    const PairLoss l = pair_loss(a, h);
+    const double g = l.slope * a.grad_scale / a.pairs;
+    slope[2 * i] = (float)(g * wc);
+    slope[2 * i + 1] = (float)(-g * wr);
+    total += l.loss;
+    if (a.margins) a.margins[i] = (float)h;
+    if (a.rewards) { a.rewards[2 * i] = (float)rc; a.rewards[2 * i + 1] = (float)rr; }
+  }
+  total = block_sum(total);      // and its barriers: the slopes are written
+  if (threadIdx.x == 0) a.loss[0] = a.pairs > 0 ? (float)(total / a.pairs) : 0.f;
+  for (int k = wave; k < 2 * a.pairs; k += 16) write_gradients(a, sequence(a.offsets, a.tokens, k), lane, 64, [&]() { return slope[k]; });
+  clear_outside(a.offsets, a.tokens, 2 * a.pairs, a.dlogp);
+}
+
+struct PolicySums { double loss, kl, clipped; uint32_t count; };      // without the tokens' weights
 
 struct PolicyArgs {
   const float *logp, *old, *ref, *advantage;
   const uint8_t* mask;
   const int64_t* offsets;
   float *loss, *kl, *clipped, *dlogp;
-  double* counts;       // [sequences][slices]: counted tokens
-  double* sums;         // [sequences * slices][3]: loss, KL, clipped tokens, weighted
+  double* sums;         // [3][sequences * slices]: loss, KL, clipped tokens
+  uint32_t* counts;     // [sequences][slices]: counted tokens
   int64_t tokens;
   int seqs, slices, by_sequence, per_token;
-  float low, high;              // bounds of the ratio
-  double log_low, log_high;     // their logarithms
+  double low, high, log_low, log_high;      // bounds of the ratio, and their logarithms
   float kl_coef, grad_scale;
 };
-
-__global__ __launch_bounds__(kThreads) void policy_counts_kernel(const PolicyArgs a) {
-  __shared__ double red[kThreads / 64];
-  const int k = blockIdx.x / a.slices, j = blockIdx.x - k * a.slices;
-  const Range r = slice(sequence(a.offsets, a.tokens, k), j, a.slices);
-  double n = 0.0;
-  if (a.mask) {
-    for (int64_t t = r.lo + threadIdx.x; t < r.hi; t += kThreads) n += a.mask[t] ? 1.0 : 0.0;
-    n = block_sum(n, red);
-  } else {
-    n = (double)(r.hi - r.lo);
-  }
-  if (threadIdx.x == 0) a.counts[blockIdx.x] = n;
-}
 
 // exp(q) - q - 1, which is q^2 / 2 and more: the series where the difference would cancel.
 __device__ inline float exp_excess(float q) {
@@ -177,67 +243,133 @@ __device__ inline float exp_excess(float q) {
   return s * q * q;
 }
 
-__global__ __launch_bounds__(kThreads) void policy_grad_kernel(const PolicyArgs a) {
-  __shared__ double red[kThreads / 64];
-  const int grads = a.seqs * a.slices;
-  if ((int)blockIdx.x == grads) return clear_outside(a.offsets, a.tokens, a.seqs, a.dlogp);
-  const int k = blockIdx.x / a.slices, j = blockIdx.x - k * a.slices;
-  // the weight of a counted token: 1 / all of them, or 1 / (those of its sequence x sequences that have any)
-  double own = 0.0, n = 0.0;
-  for (int i = 0; i < a.slices; ++i) own += a.counts[(int64_t)k * a.slices + i];
-  for (int i = threadIdx.x; i < a.seqs; i += kThreads) {
-    double c = 0.0;
-    for (int q = 0; q < a.slices; ++q) c += a.counts[(int64_t)i * a.slices + q];
-    n += a.by_sequence ? (c > 0.0 ? 1.0 : 0.0) : c;
-  }
-  n = block_sum(n, red);
-  if (a.by_sequence) n *= own;
-  const double w = n > 0.0 ? 1.0 / n : 0.0;
-  const Range r = slice(sequence(a.offsets, a.tokens, k), j, a.slices);
-  double loss = 0.0, kl = 0.0, clipped = 0.0;
-  for (int64_t t = r.lo + threadIdx.x; t < r.hi; t += kThreads) {
-    float g = 0.f;
-    if (!a.mask || a.mask[t]) {
-      const float A = a.advantage[a.per_token ? t : k];
-      // which side of a bound the ratio lies on is decided by the difference itself, in 64 bits
-      const double diff = (double)a.logp[t] - (double)a.old[t];
-      const bool over = (A > 0.f && diff > a.log_high) || (A < 0.f && diff < a.log_low);
-      const float rho = expf((float)diff);
-      const float kept = over ? (A > 0.f ? a.high : a.low) : rho;
-      float q = 0.f, excess = 0.f, slope = 0.f;
-      if (a.ref) {
-        q = (float)((double)a.ref[t] - (double)a.logp[t]);
-        excess = exp_excess(q);
-        slope = expm1f(q);
-      }
-      g = (float)w * a.grad_scale * ((over ? 0.f : -rho * A) - a.kl_coef * slope);
-      loss += (double)(a.kl_coef * excess - kept * A);
-      kl += (double)excess;
-      clipped += over ? 1.0 : 0.0;
-    }
-    a.dlogp[t] = g;
-  }
-  loss = block_sum(loss, red);
-  kl = block_sum(kl, red);
-  clipped = block_sum(clipped, red);
-  if (threadIdx.x == 0) {
-    double* o = a.sums + (int64_t)blockIdx.x * 3;
-    o[0] = loss * w; o[1] = kl * w; o[2] = clipped * w;
-  }
+// The tokens of a range: their gradients without the weight, and a thread's share of the sums.
+struct PolicyToken { float logp, old, ref, A; uint8_t on; };
+__device__ inline PolicySums policy_tokens(const PolicyArgs& a, TokenRange r, int first, int stride, int k) {
+  PolicySums s = {0.0, 0.0, 0.0, 0};
+  for_tokens(r, first, stride,
+             [&](int64_t t) {
+               return PolicyToken{a.logp[t], a.old[t], a.ref ? a.ref[t] : 0.f, a.advantage[a.per_token ? t : k],
+                                  a.mask ? a.mask[t] : (uint8_t)1};
+             },
+             [&](int64_t t, const PolicyToken& x) {
+               float g = 0.f;
+               if (x.on) {
+                 // which side of a bound the ratio lies on is decided by the difference itself, in 64 bits
+                 const double diff = (double)x.logp - (double)x.old;
+                 const bool over = (x.A > 0.f && diff > a.log_high) || (x.A < 0.f && diff < a.log_low);
+                 const float rho = expf((float)diff);
+                 const double kept = over ? (x.A > 0.f ? a.high : a.low) : (double)rho;
+                 const float q = a.ref ? (float)((double)x.ref - (double)x.logp) : 0.f, excess = exp_excess(q);
+                 g = a.grad_scale * ((over ? 0.f : -rho * x.A) - a.kl_coef * (q + excess));      // exp(q) - 1
+                 s.loss += (double)a.kl_coef * excess - kept * x.A;      // the clipped terms are all of one size: a rounding of it would add up
+                 s.kl += (double)excess;
+                 s.clipped += over ? 1.0 : 0.0;
+                 s.count += 1;
+               }
+               a.dlogp[t] = g;
+             });
+  return s;
+}
+// What the tokens' weights are made of: over all sequences their counted tokens, or how many have any (by_sequence).
+__device__ inline double share(const PolicyArgs& a, double count) { return a.by_sequence ? (count > 0.0 ? 1.0 : 0.0) : count; }
+// The weight of a counted token: 1 / all of them, or 1 / (those of its sequence x sequences that have any).
+__device__ inline double token_weight(const PolicyArgs& a, double n, double own) {
+  const double c = a.by_sequence ? n * own : n;
+  return c > 0.0 ? 1.0 / c : 0.0;
+}
+template <class W>
+__device__ inline void scale_gradients(const PolicyArgs& a, TokenRange r, int first, int stride, W weight) {
+  const int64_t t0 = r.lo + first;
+  float g[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) g[u] = t0 + (int64_t)u * stride < r.hi ? a.dlogp[t0 + (int64_t)u * stride] : 0.f;
+  const float w = weight();
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u)
+    if (t0 + (int64_t)u * stride < r.hi) a.dlogp[t0 + (int64_t)u * stride] = g[u] * w;
+  for_tokens(r, first + kAhead * stride, stride, [&](int64_t t) { return a.dlogp[t]; }, [&](int64_t t, float x) { a.dlogp[t] = x * w; });
+}
+__device__ inline void policy_results(const PolicyArgs& a, double loss, double kl, double clipped) {
+  a.loss[0] = (float)loss;
+  if (a.kl) a.kl[0] = (float)kl;
+  if (a.clipped) a.clipped[0] = (float)clipped;
 }
 
-__global__ __launch_bounds__(kThreads) void policy_total_kernel(const PolicyArgs a) {
-  __shared__ double red[kThreads / 64];
-  double s[3] = {0.0, 0.0, 0.0};
-  for (int i = threadIdx.x; i < a.seqs * a.slices; i += kThreads)
-    for (int q = 0; q < 3; ++q) s[q] += a.sums[(int64_t)i * 3 + q];
-  for (int q = 0; q < 3; ++q) s[q] = block_sum(s[q], red);
-  if (threadIdx.x == 0) {
-    a.loss[0] = (float)s[0];
-    if (a.kl) a.kl[0] = (float)s[1];
-    if (a.clipped) a.clipped[0] = (float)s[2];
-  }
+// The first launch computes everything but the weight, which needs the count of all tokens, the second one scales: 8 bytes a
+// token more than counting first and computing then, but the longer launch has nothing to wait for.  1048576 tokens: 18 us
+// where a count, the gradients and a sum of the sums took 29, and 40 where the last workgroup of the gradients summed up
+// (its device-scope ordering writes caches back).
+__global__ __launch_bounds__(kThreads) void policy_tokens_kernel(const PolicyArgs a) {
+  const int k = blockIdx.x / a.slices, j = blockIdx.x - k * a.slices;
+  const PolicySums s = policy_tokens(a, token_slice(sequence(a.offsets, a.tokens, k), j, a.slices), threadIdx.x, kThreads, k);
+  const int64_t n = (int64_t)a.seqs * a.slices;
+  double t[4] = {s.loss, s.kl, s.clipped, (double)s.count};
+  block_sums(t);
+  if (threadIdx.x != 0) return;
+  for (int q = 0; q < 3; ++q) a.sums[q * n + blockIdx.x] = t[q];
+  a.counts[blockIdx.x] = (uint32_t)t[3];
 }
+
+// Workgroup seqs * slices: the results, and the tokens of no sequence.
+__global__ __launch_bounds__(kThreads) void policy_scale_kernel(const PolicyArgs a) {
+  const int grads = a.seqs * a.slices, k = blockIdx.x / a.slices, j = blockIdx.x - k * a.slices;
+  const bool total = (int)blockIdx.x == grads;
+  auto count = [&](int i) {
+    uint32_t c = 0;
+#pragma unroll 4
+    for (int q = 0; q < a.slices; ++q) c += a.counts[i * a.slices + q];
+    return (double)c;
+  };
+  auto all = [&]() {
+    double n = 0.0;
+    for (int i = threadIdx.x; i < a.seqs; i += kThreads) n += share(a, count(i));
+    return block_sum(n);
+  };
+  if (!total) {
+    const TokenRange r = token_slice(sequence(a.offsets, a.tokens, k), j, a.slices);
+    return scale_gradients(a, r, threadIdx.x, kThreads, [&]() { return (float)token_weight(a, all(), a.by_sequence ? count(k) : 0.0); });
+  }
+  const double n = all();
+  double t[3] = {0.0, 0.0, 0.0};
+  for (int i = threadIdx.x; i < a.seqs; i += kThreads) {
+    const double w = token_weight(a, n, a.by_sequence ? count(i) : 0.0);
+#pragma unroll 2
+    for (int q = i * a.slices; q < (i + 1) * a.slices; ++q)
+      for (int m = 0; m < 3; ++m) t[m] += a.sums[(int64_t)m * grads + q] * w;
+  }
+  block_sums(t);
+  if (threadIdx.x == 0) policy_results(a, t[0], t[1], t[2]);
+  clear_outside(a.offsets, a.tokens, a.seqs, a.dlogp);
+}
+
+// A small batch in one workgroup and one launch: a wave to a sequence.
+__global__ __launch_bounds__(1024) void policy_small_kernel(const PolicyArgs a) {
+  __shared__ PolicySums sums[kSmallSeqs];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  double n = 0.0;
+  for (int k = wave; k < a.seqs; k += 16) {
+    const PolicySums s = policy_tokens(a, sequence(a.offsets, a.tokens, k), lane, 64, k);
+    const PolicySums t = {wave_sum(s.loss), wave_sum(s.kl), wave_sum(s.clipped), (uint32_t)wave_sum((double)s.count)};
+    if (lane == 0) {
+      sums[k] = t;
+      n += share(a, t.count);
+    }
+  }
+  n = block_sum(n);      // and its barriers: the sums are written
+  double t[3] = {0.0, 0.0, 0.0};
+  for (int k = wave; k < a.seqs; k += 16) {
+    const double w = token_weight(a, n, sums[k].count);
+    scale_gradients(a, sequence(a.offsets, a.tokens, k), lane, 64, [&]() { return (float)w; });
+    if (lane == 0) { t[0] += sums[k].loss * w; t[1] += sums[k].kl * w; t[2] += sums[k].clipped * w; }
+  }
+  clear_outside(a.offsets, a.tokens, a.seqs, a.dlogp);
+  block_sums(t);
+  if (threadIdx.x == 0) policy_results(a, t[0], t[1], t[2]);
+}
+
+// Whether a batch goes to one workgroup.
+bool small(int64_t tokens, int64_t sequences) { return tokens <= kSmallTokens && sequences <= kSmallSeqs; }
 
 int slices_of(int64_t tokens, int64_t sequences) {
   const int64_t mean = sequences > 0 ? tokens / sequences : 0;
@@ -283,7 +415,7 @@ void* aligned(void* ws) { return (void*)(((uintptr_t)ws + 255) / 256 * 256); }
 size_t preference_bytes(const mecefo_preference_desc_t* d) {
   return (size_t)2 * d->pairs * slices_of(d->tokens, (int64_t)d->pairs * 2) * sizeof(Part) + 256;
 }
-size_t policy_bytes(const mecefo_policy_desc_t* d) { return (size_t)d->sequences * slices_of(d->tokens, d->sequences) * 4 * sizeof(double) + 256; }
+size_t policy_bytes(const mecefo_policy_desc_t* d) { return (size_t)d->sequences * slices_of(d->tokens, d->sequences) * (3 * sizeof(double) + sizeof(uint32_t)) + 256; }
 
 }  // namespace
 }  // namespace mecefo
@@ -316,6 +448,11 @@ mecefo_status_t mecefo_preference_loss(const mecefo_preference_desc_t* desc, con
   const int slices = slices_of(desc->tokens, (int64_t)desc->pairs * 2), grads = 2 * desc->pairs * slices;
   const PrefArgs a = {logp, ref_logp, mask, offsets, loss, margins, rewards, dlogp, (Part*)aligned(ws), desc->tokens, desc->pairs,
                       slices, desc->length_mean, desc->beta, desc->label_smoothing, desc->margin, desc->grad_scale};
+  if (small(desc->tokens, (int64_t)desc->pairs * 2)) {
+    hipLaunchKernelGGL(preference_small_kernel, dim3(1), dim3(1024), 0, s, a);
+    LAUNCHED("preference_loss");
+    return MECEFO_OK;
+  }
   if (grads > 0) {
     hipLaunchKernelGGL(preference_sums_kernel, dim3(grads), dim3(kThreads), 0, s, a);
     LAUNCHED("preference_loss");
@@ -346,18 +483,20 @@ mecefo_status_t mecefo_policy_loss(const mecefo_policy_desc_t* desc, const float
   TRY(check_ws(policy_bytes(desc), ws, ws_bytes));
   hipStream_t s = (hipStream_t)hip_stream;
   const int slices = slices_of(desc->tokens, desc->sequences), grads = desc->sequences * slices;
-  double* counts = (double*)aligned(ws);
-  const PolicyArgs a = {logp, old_logp, ref_logp, advantage, mask, offsets, loss, kl, clipped, dlogp, counts, counts + grads,
-                        desc->tokens, desc->sequences, slices, desc->mean == MECEFO_MEAN_SEQUENCES, desc->advantage_per_token,
-                        (float)(1.0 - (double)desc->clip_low), (float)(1.0 + (double)desc->clip_high), log1p(-(double)desc->clip_low),
+  const PolicyArgs a = {logp, old_logp, ref_logp, advantage, mask, offsets, loss, kl, clipped, dlogp, (double*)aligned(ws),
+                        (uint32_t*)((double*)aligned(ws) + (int64_t)3 * grads), desc->tokens, desc->sequences, slices, desc->mean == MECEFO_MEAN_SEQUENCES, desc->advantage_per_token,
+                        1.0 - (double)desc->clip_low, 1.0 + (double)desc->clip_high, log1p(-(double)desc->clip_low),
                         log1p((double)desc->clip_high), desc->kl_coef, desc->grad_scale};
+  if (small(desc->tokens, desc->sequences)) {
+    hipLaunchKernelGGL(policy_small_kernel, dim3(1), dim3(1024), 0, s, a);
+    LAUNCHED("policy_loss");
+    return MECEFO_OK;
+  }
   if (grads > 0) {
-    hipLaunchKernelGGL(policy_counts_kernel, dim3(grads), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(policy_tokens_kernel, dim3(grads), dim3(kThreads), 0, s, a);
     LAUNCHED("policy_loss");
   }
-  hipLaunchKernelGGL(policy_grad_kernel, dim3(grads + 1), dim3(kThreads), 0, s, a);
-  LAUNCHED("policy_loss");
-  hipLaunchKernelGGL(policy_total_kernel, dim3(1), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(policy_scale_kernel, dim3(grads + 1), dim3(kThreads), 0, s, a);
   LAUNCHED("policy_loss");
   return MECEFO_OK;
 }

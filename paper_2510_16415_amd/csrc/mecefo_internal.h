@@ -222,6 +222,15 @@ struct Ckpt { int8_t* q; uint8_t* e; int64_t ldq, lde; };
 bool reaches_2gib(int64_t rows, int64_t ld, int esz);
 hipError_t launch_ckpt_pack(bool bf16, const void* X, int64_t ldx, int64_t rows, int cols, const Ckpt& k, hipStream_t s);
 hipError_t launch_ckpt_unpack(bool bf16, const Ckpt& k, int64_t rows, int cols, void* X, int64_t ldx, hipStream_t s);
+// launch_rmsnorm_fwd, U with row stride d, and X [rows x d] packed in the same launch.  bf16: d % 8 == 0.
+hipError_t launch_rmsnorm_pack(bool bf16, const void* X, int64_t ldx, const void* gamma, float eps, void* U, float* rstd, int64_t rows,
+                               int d, const Ckpt& k, hipStream_t s);
+// H [rows x d] = the checkpoint's values, U = norm(H) gamma, rstd: what unpacking and launch_rmsnorm_fwd give.  bf16: d % 8 == 0.
+hipError_t launch_rmsnorm_ckpt(bool bf16, const Ckpt& k, const void* gamma, float eps, void* H, void* U, float* rstd, int64_t rows, int d,
+                               hipStream_t s);
+// launch_swiglu_bwd with G and Z as checkpoints; ldf a multiple of 8, all of it padded.
+hipError_t launch_swiglu_bwd_ckpt(bool bf16, const Ckpt& G, const Ckpt& Z, void* DG, void* DZ, void* AA, int64_t ldf, int64_t b, int f,
+                                  hipStream_t s);
 
 
 // Fused causal attention forward: O = softmax(scale Q K^T) V and the row log-sum-exp L [batch*heads][seq],
