@@ -260,13 +260,14 @@ template <class F> __device__ inline float row16(float v, F f) {
 
 // EPI_HEAD_LSE of a wave's accumulators, without LDS: element e of block (i, j) is row 16 i + 4 (lane / 16) + e, column
 // 16 j + lane % 16 of the wave's part, so a row is TN values in each of 16 lanes.  The 4 TM rows of a lane are handed to its
-// 16-lane row, one to a lane, and 16 of them go out in one store.
-template <int TM, int TN>
-__device__ inline void head_lse(const GemmProblem& p, const f32x4_t (&acc)[TM][TN], int row_w, int col_w, int lane) {
-  if (col_w >= p.N) return;
-  const int64_t* labels = (const int64_t*)p.C[1];
+// 16-lane row, one to a lane, and 16 of them go out in one store.  With z' = z log2(e) = acc * k an element takes a third of a
+// max3, a fused multiply-add, an exponential (four issue slots) and an add; the largest acc gives the largest z', or the
+// smallest one where k is negative (UP).  EDGE: some of the columns are behind the matrix.
+template <int TM, int TN, bool UP, bool EDGE>
+__device__ inline void head_lse_rows(const GemmProblem& p, const f32x4_t (&acc)[TM][TN], int row_w, int col_w, int lane, float k) {
   float2* out = (float2*)p.C[0] + (int64_t)(col_w / (16 * TN)) * p.ldc;
   const int c0 = lane & 15, left = p.N - col_w;
+  constexpr float kNone = UP ? -INFINITY : INFINITY;
 #pragma unroll
   for (int i0 = 0; i0 < TM; i0 += 4) {
     float2 mine = {0.f, 0.f};
@@ -274,30 +275,63 @@ __device__ inline void head_lse(const GemmProblem& p, const f32x4_t (&acc)[TM][T
     for (int i = i0; i < TM && i < i0 + 4; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float z[TN], m = -INFINITY;
+        float m = kNone;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-          z[j] = 16 * j + c0 < left ? acc[i][j][e] * p.scale : -INFINITY;
-          m = fmaxf(m, z[j]);
+          const float v = !EDGE || 16 * j + c0 < left ? acc[i][j][e] : kNone;
+          m = UP ? fmaxf(m, v) : fminf(m, v);
         }
-        m = row16(m, [](float a, float b) { return fmaxf(a, b); });
+        m = row16(m, [](float x, float y) { return UP ? fmaxf(x, y) : fminf(x, y); });
+        const float top = m * k;
         float s = 0.f;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) s += __builtin_amdgcn_exp2f(1.44269504088896341f * (z[j] - m));
-        s = row16(s, [](float a, float b) { return a + b; });
-        if (c0 == 4 * (i - i0) + e) mine = float2{m, s};
-        const int row = row_w + 16 * i + 4 * (lane >> 4) + e;
-        const int64_t at = (row < p.M ? labels[row] : -1) - col_w;
-        if (at >= 0 && at < left && at < 16 * TN && (int)(at & 15) == c0) {      // one lane of the launch
-          float zl = z[0];
-#pragma unroll
-          for (int j = 1; j < TN; ++j) zl = (int)(at >> 4) == j ? z[j] : zl;
-          ((float*)p.C[2])[row] = zl;
+        for (int j = 0; j < TN; ++j) {
+          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], k, -top));
+          s += !EDGE || 16 * j + c0 < left ? x : 0.f;
         }
+        s = row16(s, [](float x, float y) { return x + y; });
+        if (c0 == 4 * (i - i0) + e) mine = float2{top, s};
       }
     const int row = row_w + 16 * (i0 + (c0 >> 2)) + 4 * (lane >> 4) + (c0 & 3);
     if (i0 + (c0 >> 2) < TM && row < p.M) out[row] = mine;
   }
+}
+
+// z at the labels of the wave's rows that fall into its columns: few waves have any.
+template <int TM, int TN>
+__device__ inline void head_labels(const GemmProblem& p, const f32x4_t (&acc)[TM][TN], int row_w, int col_w, int lane) {
+  const int64_t* labels = (const int64_t*)p.C[1];
+  const int c0 = lane & 15, left = p.N - col_w < 16 * TN ? p.N - col_w : 16 * TN;
+  bool any = false;
+  for (int r = lane; r < 16 * TM; r += 64) {
+    const int64_t at = (row_w + r < p.M ? labels[row_w + r] : -1) - col_w;
+    any |= at >= 0 && at < left;
+  }
+  if (!__any(any)) return;
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int row = row_w + 16 * i + 4 * (lane >> 4) + e;
+      const int64_t at = (row < p.M ? labels[row] : -1) - col_w;
+      if (at >= 0 && at < left && (int)(at & 15) == c0) {
+        float v = acc[i][0][e];
+#pragma unroll
+        for (int j = 1; j < TN; ++j) v = (int)(at >> 4) == j ? acc[i][j][e] : v;
+        ((float*)p.C[2])[row] = v * p.scale;
+      }
+    }
+}
+
+template <int TM, int TN>
+__device__ inline void head_lse(const GemmProblem& p, const f32x4_t (&acc)[TM][TN], int row_w, int col_w, int lane) {
+  if (col_w >= p.N) return;
+  const float k = p.scale * kLog2e;
+  const bool edge = col_w + 16 * TN > p.N;
+  if (k < 0.f) head_lse_rows<TM, TN, false, true>(p, acc, row_w, col_w, lane, k);
+  else if (edge) head_lse_rows<TM, TN, true, true>(p, acc, row_w, col_w, lane, k);
+  else head_lse_rows<TM, TN, true, false>(p, acc, row_w, col_w, lane, k);
+  head_labels<TM, TN>(p, acc, row_w, col_w, lane);
 }
 
 // RAGGED: K may end inside a 16-byte chunk (the instantiation without it keeps the large tile's loop free of the

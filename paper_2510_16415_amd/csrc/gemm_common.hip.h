@@ -341,6 +341,8 @@ __device__ inline void causal_clip(const GemmProblem& p, int m0, int n0, int bm,
 template <typename T> __device__ inline float to_f32(T x) { return (float)x; }
 template <typename T> __device__ inline T from_f32(float x) { return (T)x; }
 
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
 // silu(g) and its derivative.  PRECISE (fp32 storage path) uses expf and a true divide;
 // the bf16 path uses the hardware exp2/rcp approximations, far below bf16 resolution.
 template <bool PRECISE> __device__ inline float sigmoid_f(float g) {
@@ -545,11 +547,18 @@ __device__ inline void epilogue_vec8(const GemmProblem& p, const KHead& a, int s
     *c = pack_bf16x8(o);
   } else if constexpr (EPI == EPI_HEAD_GRAD) {
     const HeadRow h = head_row(p, row);
+    const float k = p.scale * kLog2e, l = h.lse * kLog2e;
     float o[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float pr = __builtin_amdgcn_exp2f(1.44269504088896341f * (v[e] * p.scale - h.lse));
-      o[e] = h.c == 0.f ? 0.f : h.c * ((h.label == col0 + e ? 1.f : 0.f) - pr);
+    for (int e = 0; e < 8; ++e) o[e] = -h.c * __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], k, -l));
+    const int at = h.label - col0;
+    if (at >= 0 && at < 8) {      // few rows have their label here
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = at == e ? h.c + o[e] : o[e];
+    }
+    if (h.c == 0.f) {             // also where the exponential is not finite
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = 0.f;
     }
     *(bf16x8s_t*)((__bf16*)p.C[0] + idx) = pack_bf16x8(o);
   } else if constexpr (EPI == EPI_GRAD) {      // bf16 gradients; fp32 ones take epilogue_vec4

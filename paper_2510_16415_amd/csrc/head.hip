@@ -53,8 +53,8 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(const float* __restrict
   if (lse) lse[row] = l;
 }
 
-// lse and logp from the parts that the products' epilogue leaves: (largest z, sum of exp(z - that)) of a row over part_cols
-// columns, [parts][rows], and z at the label.  ROWS neighbouring rows to a workgroup, 1024 / ROWS threads share out a row's
+// lse and logp from the parts that the products' epilogue leaves: (largest z', sum of 2^(z' - that)) of a row over part_cols
+// columns, [parts][rows], z' = z log2(e), and z at the label.  ROWS neighbouring rows to a workgroup, 1024 / ROWS threads share out a row's
 // parts: 16 rows read whole lines, where there are few rows 2 use more of the chip (77 rows of 500 parts: HEAD_PARTS us).
 template <int ROWS>
 __global__ __launch_bounds__(1024) void head_parts_kernel(const float2* __restrict__ part, int parts, int rows, int vocab,
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(1024) void head_parts_kernel(const float2* __restri
   const int r = threadIdx.x % ROWS, g = threadIdx.x / ROWS, row = blockIdx.x * ROWS + r;
   auto join = [](float2 x, float2 y) {      // a share without parts is (-inf, 0)
     const float m = fmaxf(x.x, y.x), k = m == -INFINITY ? 0.f : m;
-    return float2{m, x.y * __builtin_amdgcn_exp2f(1.44269504088896341f * (x.x - k)) + y.y * __builtin_amdgcn_exp2f(1.44269504088896341f * (y.x - k))};
+    return float2{m, x.y * __builtin_amdgcn_exp2f(x.x - k) + y.y * __builtin_amdgcn_exp2f(y.x - k)};
   };
   float2 a = {-INFINITY, 0.f};
   const int at = row < rows ? row : rows - 1;
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(1024) void head_parts_kernel(const float2* __restri
   if (threadIdx.x >= ROWS || row >= rows) return;
 #pragma unroll
   for (int w = 1; w < 16; ++w) a = join(a, red[w][r]);
-  const float l = a.x + logf(a.y);
+  const float l = a.x * kLn2 + logf(a.y);
   logp[row] = counted(labels[row], vocab) ? zl[row] - l : 0.f;
   if (lse) lse[row] = l;
 }

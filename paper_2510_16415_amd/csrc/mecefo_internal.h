@@ -19,8 +19,8 @@ enum Epilogue : int {
                        // fold_norm (bf16): x = acc / (norm of a matrix whose kNormBlocks parts have the norms in rowvec)
   EPI_RESID = 9,       // C0[row, col] = acc + C1[row, col]   (activation dtype; C1 may be C0)
   EPI_ROPE = 10,       // C0 = acc rotated: pairs (j, j + rope_half) of every head by the angle of position row % rope_seq
-  EPI_HEAD_LSE = 11,   // z = scale * acc is not stored: C0 (fp32 pairs [columns / part_cols][ldc]) = the largest z of a row over part_cols
-                       // columns and the sum of exp(z - that); C2 (fp32) [row] = z at the row's label, C1 (int64)   (bf16, NT)
+  EPI_HEAD_LSE = 11,   // z = scale * acc is not stored: C0 (fp32 pairs [columns / part_cols][ldc]) = the largest z' = z log2(e) of a row
+                       // over part_cols columns and the sum of 2^(z' - that); C2 (fp32) [row] = z at the row's label, C1 (int64)   (bf16, NT)
   EPI_HEAD_GRAD = 12,  // C0[row, col] = scale * addend[row] * ([col = label] - exp(scale * acc - rowvec[row])), 0 where the label C1[row]
                        // (int64) is no column; columns [N, pad_cols) are set to zero   (NT)
 };
