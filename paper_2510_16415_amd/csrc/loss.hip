@@ -15,10 +15,16 @@ namespace mecefo {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSliceTokens = 1024;   // tokens of a slice, in a sequence of mean length
-constexpr int kMaxSlices = 64;
-constexpr int kWaveSlices = 16;
-constexpr int kSmallTokens = 4096, kSmallSeqs = 512;
+// Slices of a sequence of mean length: of 512 tokens or more, and about four workgroups a CU.  Preference / policy with slices of
+// 512 / 1024 / 2048 tokens, us: 128 sequences of 4096 tokens 10.8, 12.9 / 12.1, 14.8 / 17.9, 22.1; 512 of 2048 14.9, 20.4 / 14.0, 19.2 /
+// 18.8, 24.0; 8 of 1000 6.9, 8.7 / 8.3, 9.8 / 8.4, 9.8.
+constexpr int kSliceTokens = 512;
+constexpr int kMaxSlices = 256;
+constexpr int kWaveSlices = 16;      // from here on a wave adds up a sequence's slices, below a thread does
+// One workgroup and one launch: a wave to a sequence.  GPU time of one launch / two, us: preference 8 x 64 tokens 6.0 / 6.6, 8 x 250
+// 7.5 / 6.6, 64 x 16 13.1 / 6.7, 512 x 8 72 / 7.7; policy 2 x 100 8.1 / 7.5.  Calls that a program makes one by one, the launches among
+// them: preference 2 x 20 to 16 x 32 7.6 to 8.1 / 11.4, policy 8.0 to 10 / 11.5.
+constexpr int kSmallTokens = 512, kSmallSeqs = 16;
 
 struct Part { double sum; double count; };
 
@@ -77,11 +83,17 @@ struct PrefArgs {
   double beta, smooth, margin, grad_scale;
 };
 
-// The slices of one sequence added up, by one wave (slices <= 64), in all its lanes.
-__device__ inline Part add_slices(const Part* p, int n) {
-  const int lane = threadIdx.x & 63;
-  const Part x = lane < n ? p[lane] : Part{0.0, 0.0};
-  return Part{wave_sum(x.sum), wave_sum(x.count)};
+// The slices of one sequence added up by a wave, in all its lanes, or by a thread.
+__device__ inline Part wave_slices(const Part* p, int n) {
+  Part s = {0.0, 0.0};
+  for (int j = threadIdx.x & 63; j < n; j += 64) { s.sum += p[j].sum; s.count += p[j].count; }
+  return Part{wave_sum(s.sum), wave_sum(s.count)};
+}
+__device__ inline Part thread_slices(const Part* p, int n) {
+  Part s = {0.0, 0.0};
+#pragma unroll 4
+  for (int j = 0; j < n; ++j) { const Part x = p[j]; s.sum += x.sum; s.count += x.count; }
+  return s;
 }
 // Sum over a range of the counted tokens' log ratios, and how many there are, a thread's share.
 struct Ratio { float logp, ref; uint8_t on; };
@@ -150,22 +162,16 @@ __global__ __launch_bounds__(kThreads) void preference_grad_kernel(const PrefArg
       if (a.margins) a.margins[i] = (float)h;
       if (a.rewards) { a.rewards[2 * i] = (float)rc; a.rewards[2 * i + 1] = (float)rr; }
     };
-    if (a.slices >= kWaveSlices) {
+    const Part* parts = a.parts;
+    const int n = a.slices;
+    if (n >= kWaveSlices) {
       for (int i = threadIdx.x >> 6; i < a.pairs; i += kThreads / 64) {
-        const Part c = add_slices(a.parts + (int64_t)(2 * i) * a.slices, a.slices), o = add_slices(a.parts + (int64_t)(2 * i + 1) * a.slices, a.slices);
+        const Part c = wave_slices(parts + (int64_t)(2 * i) * n, n), o = wave_slices(parts + (int64_t)(2 * i + 1) * n, n);
         if ((threadIdx.x & 63) == 0) pair(i, c, o);
       }
     } else {
-      for (int i = threadIdx.x; i < a.pairs; i += kThreads) {
-        Part p[2] = {{0.0, 0.0}, {0.0, 0.0}};
-        for (int k = 0; k < 2; ++k)
-#pragma unroll 4
-          for (int j = 0; j < a.slices; ++j) {
-            const Part x = a.parts[(int64_t)(2 * i + k) * a.slices + j];
-            p[k].sum += x.sum; p[k].count += x.count;
-          }
-        pair(i, p[0], p[1]);
-      }
+      for (int i = threadIdx.x; i < a.pairs; i += kThreads)
+        pair(i, thread_slices(parts + (int64_t)(2 * i) * n, n), thread_slices(parts + (int64_t)(2 * i + 1) * n, n));
     }
     total = block_sum(total);
     if (threadIdx.x == 0) a.loss[0] = a.pairs > 0 ? (float)(total / a.pairs) : 0.f;
@@ -177,7 +183,7 @@ __global__ __launch_bounds__(kThreads) void preference_grad_kernel(const PrefArg
   write_gradients(a, r, threadIdx.x, kThreads, [&]() {
     double wc, wr;
     const int c = k & ~1;
-    const Part pc = add_slices(a.parts + (int64_t)c * a.slices, a.slices), pr = add_slices(a.parts + (int64_t)(c + 1) * a.slices, a.slices);
+    const Part pc = wave_slices(a.parts + (int64_t)c * a.slices, a.slices), pr = wave_slices(a.parts + (int64_t)(c + 1) * a.slices, a.slices);
     const double rc = reward(a, pc, &wc), rr = reward(a, pr, &wr);
     const double g = pair_loss(a, rc - rr - a.margin).slope * a.grad_scale / a.pairs;
     return (float)(k & 1 ? -g * wr : g * wc);
@@ -297,7 +303,7 @@ __device__ inline void policy_results(const PolicyArgs& a, double loss, double k
 }
 
 // The first launch computes everything but the weight, which needs the count of all tokens, the second one scales: 8 bytes a
-// token more than counting first and computing then, but the longer launch has nothing to wait for.  1048576 tokens: 18 us
+// token more than counting first and computing then, but the longer launch has nothing to wait for.  1048576 tokens: 19 us
 // where a count, the gradients and a sum of the sums took 29, and 40 where the last workgroup of the gradients summed up
 // (its device-scope ordering writes caches back).
 __global__ __launch_bounds__(kThreads) void policy_tokens_kernel(const PolicyArgs a) {
@@ -313,30 +319,55 @@ __global__ __launch_bounds__(kThreads) void policy_tokens_kernel(const PolicyArg
 
 // Workgroup seqs * slices: the results, and the tokens of no sequence.
 __global__ __launch_bounds__(kThreads) void policy_scale_kernel(const PolicyArgs a) {
-  const int grads = a.seqs * a.slices, k = blockIdx.x / a.slices, j = blockIdx.x - k * a.slices;
-  const bool total = (int)blockIdx.x == grads;
-  auto count = [&](int i) {
+  const int grads = a.seqs * a.slices, k = blockIdx.x / a.slices, j = blockIdx.x - k * a.slices, lane = threadIdx.x & 63;
+  const bool total = (int)blockIdx.x == grads, waves = a.slices >= kWaveSlices;
+  auto wave_count = [&](int i) {
+    double c = 0.0;
+    for (int q = lane; q < a.slices; q += 64) c += a.counts[i * a.slices + q];
+    return wave_sum(c);
+  };
+  auto thread_count = [&](int i) {
     uint32_t c = 0;
 #pragma unroll 4
     for (int q = 0; q < a.slices; ++q) c += a.counts[i * a.slices + q];
     return (double)c;
   };
+  // all counted tokens, or the sequences that have any
   auto all = [&]() {
     double n = 0.0;
-    for (int i = threadIdx.x; i < a.seqs; i += kThreads) n += share(a, count(i));
+    if (!a.by_sequence) {
+      for (int i = threadIdx.x; i < grads; i += kThreads) n += a.counts[i];
+    } else if (waves) {
+      for (int i = threadIdx.x >> 6; i < a.seqs; i += kThreads / 64) n += wave_count(i) > 0.0 && lane == 0 ? 1.0 : 0.0;
+    } else {
+      for (int i = threadIdx.x; i < a.seqs; i += kThreads) n += thread_count(i) > 0.0 ? 1.0 : 0.0;
+    }
     return block_sum(n);
   };
   if (!total) {
     const TokenRange r = token_slice(sequence(a.offsets, a.tokens, k), j, a.slices);
-    return scale_gradients(a, r, threadIdx.x, kThreads, [&]() { return (float)token_weight(a, all(), a.by_sequence ? count(k) : 0.0); });
+    return scale_gradients(a, r, threadIdx.x, kThreads, [&]() { return (float)token_weight(a, all(), a.by_sequence ? wave_count(k) : 0.0); });
   }
   const double n = all();
   double t[3] = {0.0, 0.0, 0.0};
-  for (int i = threadIdx.x; i < a.seqs; i += kThreads) {
-    const double w = token_weight(a, n, a.by_sequence ? count(i) : 0.0);
+  auto add = [&](int q, double w) {
+    for (int m = 0; m < 3; ++m) t[m] += a.sums[(int64_t)m * grads + q] * w;
+  };
+  if (!a.by_sequence) {
+    const double w = token_weight(a, n, 0.0);
 #pragma unroll 2
-    for (int q = i * a.slices; q < (i + 1) * a.slices; ++q)
-      for (int m = 0; m < 3; ++m) t[m] += a.sums[(int64_t)m * grads + q] * w;
+    for (int q = threadIdx.x; q < grads; q += kThreads) add(q, w);
+  } else if (waves) {
+    for (int i = threadIdx.x >> 6; i < a.seqs; i += kThreads / 64) {
+      const double w = token_weight(a, n, wave_count(i));
+      for (int q = lane; q < a.slices; q += 64) add(i * a.slices + q, w);
+    }
+  } else {
+    for (int i = threadIdx.x; i < a.seqs; i += kThreads) {
+      const double w = token_weight(a, n, thread_count(i));
+#pragma unroll 2
+      for (int q = 0; q < a.slices; ++q) add(i * a.slices + q, w);
+    }
   }
   block_sums(t);
   if (threadIdx.x == 0) policy_results(a, t[0], t[1], t[2]);
@@ -373,7 +404,7 @@ bool small(int64_t tokens, int64_t sequences) { return tokens <= kSmallTokens &&
 
 int slices_of(int64_t tokens, int64_t sequences) {
   const int64_t mean = sequences > 0 ? tokens / sequences : 0;
-  const int64_t n = (mean + kSliceTokens - 1) / kSliceTokens;
+  const int64_t least = tokens / (4 * kCUs), size = least > kSliceTokens ? least : kSliceTokens, n = (mean + size - 1) / size;
   return (int)(n < 1 ? 1 : n > kMaxSlices ? kMaxSlices : n);
 }
 
