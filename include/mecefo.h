@@ -406,7 +406,9 @@ mecefo_status_t mecefo_stack_bwd_skip_ckpt(const mecefo_ffn_desc_t* desc, int n_
  *   U = RMSNorm(X) * gamma, or X itself where gamma is NULL;  z = logit_scale * U W^T [b x V], W [V x d] (ld_w);
  *   lse_i = log sum_v exp(z_iv);  logp_i = z_i,labels[i] - lse_i.
  * A label outside [0, vocab) marks a token that is not scored: its logp is 0 (its lse is that of its row) and it has no
- * part in the gradient, as far as its row of X is finite.
+ * part in the gradient, nor has one whose dlogp is 0 (its row of X has to be finite all the same).  Large bf16 backwards leave such
+ * rows out of their products; which rows these are is read on the device, so a captured graph follows the labels and dlogp of
+ * each replay.
  * The logits are never stored by the forward.  dtype MECEFO_BF16: products accumulated in fp32, exponentials and their
  * sums in fp32; with gamma, U is rounded to bf16.  d_model must be a multiple of 8, vocab may be any size.
  * The backward forms the products again and stores dz_iv = logit_scale * dlogp_i * ([v = labels[i]] - exp(z_iv - lse_i)) in
@@ -530,7 +532,8 @@ mecefo_status_t mecefo_init(void);
  * "S4" (128x128 with four), "T" (64x64), "T2" (64x64, two groups of waves share out K), "X" (32x32, eight waves share out K), "K" (192x256, where it is
  * built for the launch), "L8" (256x256) and "LT" ("L8" with a short last round cut up), or register-staged "L4" and "L8R"
  * (256x256); launches that a value is not built for take "L8".  name "attention": "auto" | "gemm" (batched GEMM
- * launches instead of the fused attention kernels).  Affects calls made after it returns. */
+ * launches instead of the fused attention kernels).  name "head": "auto" | "all" | "scored" (rows of the head's backward: all, or by a list of
+ * those that take part; the workspace query and the call consult the same switch).  Affects calls made after it returns. */
 mecefo_status_t mecefo_set_option(const char* name, const char* value);
 
 /* Description of the last non-OK status returned on this thread ("" if none). */

@@ -878,6 +878,12 @@ mecefo_status_t mecefo_set_option(const char* name, const char* value) {
     if (!strcmp(value, "gemm")) { options().attn_gemm.store(1, std::memory_order_relaxed); return MECEFO_OK; }
     return fail(MECEFO_ERR_INVALID_ARG, "option attention: value must be auto or gemm (got %s)", value);
   }
+  if (!strcmp(name, "head")) {
+    static const char* const kRows[3] = {"auto", "all", "scored"};
+    for (int i = 0; i < 3; ++i)
+      if (!strcmp(value, kRows[i])) { options().head_rows.store(i, std::memory_order_relaxed); return MECEFO_OK; }
+    return fail(MECEFO_ERR_INVALID_ARG, "option head: value must be auto, all or scored (got %s)", value);
+  }
   return fail(MECEFO_ERR_INVALID_ARG, "unknown option %s", name);
 }
 

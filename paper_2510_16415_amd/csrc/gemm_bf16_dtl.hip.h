@@ -565,7 +565,7 @@ __device__ __forceinline__ void dtl_tile(const KHead& head, GemmProblem p, int m
       // pieces (with eight columns per lane each of the two 16-byte stores would fill every other
       // 16 bytes of its lines)
       constexpr bool F32_OUT = EPI == EPI_HILO;
-      if constexpr (F32_OUT || EPI == EPI_GRAD || EPI == EPI_STORE) {
+      if constexpr (F32_OUT || EPI == EPI_GRAD || EPI == EPI_STORE || EPI == EPI_HEAD_DU) {
         if (F32_OUT || (EPI == EPI_GRAD ? head.out_f32 != 0 : p.splits > 1)) {
           constexpr int LPR4 = W / 4, RPI4 = 64 / LPR4;
           const int r4 = lane / LPR4, c4 = (lane % LPR4) * 4;
@@ -574,7 +574,7 @@ __device__ __forceinline__ void dtl_tile(const KHead& head, GemmProblem p, int m
             const int rl = it * RPI4 + r4;
             const f32x4_t g = *(const f32x4_t*)(ep + rl * RS + c4);
             const float v4[4] = {g[0], g[1], g[2], g[3]};
-            epilogue_vec4<EPI>(p, head, split, row_w + i * 32 + rl, col_w - rd_c8 + c4, v4);
+            epilogue_vec4<EPI == EPI_HEAD_DU ? EPI_STORE : EPI>(p, head, split, row_w + i * 32 + rl, col_w - rd_c8 + c4, v4);
           }
           continue;
         }
@@ -621,6 +621,15 @@ struct WorkgroupClock {
   }
 };
 
+// Products whose rows are counted on the device.
+constexpr bool limits_m(int epi) { return epi == EPI_HEAD_GRAD || epi == EPI_HEAD_DU; }
+constexpr bool limits_k(int epi) { return epi == EPI_HEAD_DW; }
+constexpr int tile_epi(int epi) { return epi == EPI_HEAD_DW ? EPI_GRAD : epi; }
+__device__ inline int limited(const KProblem& p, int most) {
+  const int* n = (const int*)p.C[2];
+  return n ? min(most, __builtin_amdgcn_readfirstlane(*n)) : most;
+}
+
 template <class Cfg, class Pipe, bool AKC, bool BKC, int EPI, bool RAGGED>
 __global__ __launch_bounds__(Pipe::THREADS, 2) void gemm_bf16_dtl_kernel(const KArgs args) {
   constexpr int BM = Cfg::BM, BN_OUT = epi_is_dual(EPI) ? Cfg::BN / 2 : Cfg::BN;
@@ -636,12 +645,23 @@ __global__ __launch_bounds__(Pipe::THREADS, 2) void gemm_bf16_dtl_kernel(const K
   clock.start(head);
   int index;
   const int prob = map_problem(head, blockIdx.x, &index);
-  const KProblem kp = load_problem(prob);
+  KProblem kp = load_problem(prob);
+  if constexpr (limits_k(EPI)) kp.K = limited(kp, kp.K);
+  if constexpr (limits_m(EPI)) {      // one problem; the tiles that there are, shared out over the XCDs anew
+    const int m = limited(kp, kp.M);
+    if (m < kp.M) {
+      const int per = (uint32_t)(m + BM - 1) / BM * ((uint32_t)(kp.N + BN_OUT - 1) / BN_OUT), total = per * (kp.splits_kpad >> 1);
+      if ((int)blockIdx.x >= total) return;
+      index = xcd_remap(blockIdx.x, total);
+      kp.M = m;
+      kp.by_tiles = per > 1 ? (uint32_t)(((uint64_t)1 << 32) / per + 1) : 0xFFFFFFFFu;      // div_magic
+    }
+  }
   const TileCoord tc = map_tile<BM, BN_OUT>(head, kp, prob, index);
   const GemmProblem p = product_view<2>(head, kp, tc.z);
   const int m0 = tc.tm * BM, n0 = tc.tn * BN_OUT;
   if (causal_tile_unused(p, m0, n0, BM)) return;
-  dtl_tile<Cfg, Pipe, AKC, BKC, EPI, RAGGED, true>(head, p, m0, n0, tc.split, smem);
+  dtl_tile<Cfg, Pipe, AKC, BKC, tile_epi(EPI), RAGGED, true>(head, p, m0, n0, tc.split, smem);
   clock.stop(head);
 }
 
@@ -669,6 +689,7 @@ __global__ __launch_bounds__(P2::THREADS, 2) void gemm_bf16_pair_kernel(const KA
 // last of the problem with the most.
 template <class Cfg, class Pipe, class C2, class P2, class C4, class P4, class C16, class P16, bool AKC, bool BKC, int EPI>
 __global__ __launch_bounds__(Pipe::THREADS, 2) void gemm_bf16_tail_kernel(const KArgs args) {
+  constexpr int E = tile_epi(EPI);
   static_assert(P2::THREADS == Pipe::THREADS && P4::THREADS == Pipe::THREADS && P16::THREADS == Pipe::THREADS, "one launch");
   constexpr int BM = Cfg::BM, BN_OUT = epi_is_dual(EPI) ? Cfg::BN / 2 : Cfg::BN;
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
@@ -685,31 +706,33 @@ __global__ __launch_bounds__(Pipe::THREADS, 2) void gemm_bf16_tail_kernel(const 
   if (extra < 0) {
     int index;
     const int prob = map_problem(head, bid, &index);
-    const KProblem kp = load_problem(prob);
+    KProblem kp = load_problem(prob);
+    if constexpr (limits_k(EPI)) kp.K = limited(kp, kp.K);
     const TileCoord tc = map_tile<BM, BN_OUT>(head, kp, prob, index);
     const GemmProblem p = product_view<2>(head, kp, 0);
-    dtl_tile<Cfg, Pipe, AKC, BKC, EPI, false, false>(head, p, tc.tm * BM, tc.tn * BN_OUT, 0, smem);
+    dtl_tile<Cfg, Pipe, AKC, BKC, E, false, false>(head, p, tc.tm * BM, tc.tn * BN_OUT, 0, smem);
     clock.stop(head);
     return;
   }
   const int prob = head.tail >> 28, shift = head.tail >> 24 & 15, first = head.tail & 0xFFFFFF;
   const int e = xcd_remap(extra, head.gemm_blocks - head.total);
-  const KProblem kp = load_problem(prob);
+  KProblem kp = load_problem(prob);
+  if constexpr (limits_k(EPI)) kp.K = limited(kp, kp.K);
   const TileCoord tc = map_tile<BM, BN_OUT>(head, kp, prob, first + (e >> shift));
   const GemmProblem p = product_view<2>(head, kp, 0);
   const int part = e & ((1 << shift) - 1);
   int m0 = tc.tm * BM, n0 = tc.tn * BN_OUT;
   if (shift == 1) {
     m0 += part * C2::BM;
-    if (m0 < p.M) dtl_tile<C2, P2, AKC, BKC, EPI, false, false>(head, p, m0, n0, 0, smem);
+    if (m0 < p.M) dtl_tile<C2, P2, AKC, BKC, E, false, false>(head, p, m0, n0, 0, smem);
   } else if (shift == 2) {
     m0 += (part >> 1) * C4::BM;
     n0 += (part & 1) * (BN_OUT / 2);
-    if (m0 < p.M && n0 < p.N) dtl_tile<C4, P4, AKC, BKC, EPI, false, false>(head, p, m0, n0, 0, smem);
+    if (m0 < p.M && n0 < p.N) dtl_tile<C4, P4, AKC, BKC, E, false, false>(head, p, m0, n0, 0, smem);
   } else {
     m0 += (part >> 2) * C16::BM;
     n0 += (part & 3) * (BN_OUT / 4);
-    if (m0 < p.M && n0 < p.N) dtl_tile<C16, P16, AKC, BKC, EPI, false, false>(head, p, m0, n0, 0, smem);
+    if (m0 < p.M && n0 < p.N) dtl_tile<C16, P16, AKC, BKC, E, false, false>(head, p, m0, n0, 0, smem);
   }
 }
 

@@ -84,11 +84,12 @@ inline const TileModel& tile_model(int c) {
 // What the 192-row tile and the cut-up last round are built for: operands whose rows can be cut anywhere, and the
 // epilogues of launches that can be large.
 constexpr bool has_tile_k(bool akc, bool bkc, int epi) {
-  return akc && (epi == EPI_STORE || (bkc && (epi == EPI_GRAD || epi == EPI_SWIGLU_FWD || epi == EPI_SWIGLU_BWD || epi == EPI_RESID || epi == EPI_HEAD_LSE || epi == EPI_HEAD_GRAD)));
+  return akc && (epi == EPI_STORE || epi == EPI_HEAD_DU || (bkc && (epi == EPI_GRAD || epi == EPI_SWIGLU_FWD || epi == EPI_SWIGLU_BWD || epi == EPI_RESID || epi == EPI_HEAD_LSE || epi == EPI_HEAD_GRAD)));
 }
 constexpr bool has_tile_x(int epi) { return epi != EPI_ATTN_P && epi != EPI_ATTN_DS && epi != EPI_ROPE; }
 constexpr bool has_tail(bool akc, bool bkc, int epi) {
-  return (has_tile_k(akc, bkc, epi) && epi != EPI_HEAD_LSE) || (!akc && !bkc && (epi == EPI_GRAD || epi == EPI_STORE));
+  return (has_tile_k(akc, bkc, epi) && epi != EPI_HEAD_LSE && epi != EPI_HEAD_DU) ||
+         (!akc && !bkc && (epi == EPI_GRAD || epi == EPI_STORE || epi == EPI_HEAD_DW));
 }
 
 // K stages of a workgroup of problem i, and the workgroups of the problem on bm x bn tiles.
@@ -129,6 +130,7 @@ struct TailPlan { int tiles, shift, prob; float saved; };
 inline TailPlan bf16_tail(const GemmLaunch& g, bool forced = false) {
   TailPlan plan = {0, 0, 0, 0.f};
   if (!has_tail(g.a_kcontig, g.b_kcontig, g.epi) || bf16_ragged(g)) return plan;
+  if (g.epi == EPI_HEAD_GRAD && g.p[0].C[2]) return plan;      // which tiles are the last is not known here
   int total = 0, most = 0;
   for (int i = 0; i < g.nprob; ++i) {
     const GemmProblem& p = g.p[i];
@@ -142,7 +144,7 @@ inline TailPlan bf16_tail(const GemmLaunch& g, bool forced = false) {
   const float st = (float)bf16_stages(g, 0), rate[3] = {1.0f, 0.72f, 0.45f};
   const int shift[3] = {1, 2, 4}, rounds = total / kCUs;
   float lost = 0.f;
-  if (g.epi == EPI_GRAD && st < 24.f && !forced) {
+  if ((g.epi == EPI_GRAD || g.epi == EPI_HEAD_DW) && st < 24.f && !forced) {
     if (rounds > 2) return plan;
     lost = g.out_f32 ? 4.f + 0.08f * rest + 1.2f * rounds : 2.f + 0.03f * rest + 0.5f * rounds;
   }
@@ -359,7 +361,7 @@ hipError_t run_bf16_tail(GemmLaunch& g, const TailPlan& plan, hipStream_t stream
 // the residual adds, the rotation and the head are not built for them, and such launches take the 256 x 256 direct-to-LDS tile
 // where a register-staged one is forced.
 constexpr bool register_staged(int epi) {
-  return epi != EPI_POLY && epi != EPI_HILO && epi != EPI_RESID && epi != EPI_ROPE && epi != EPI_HEAD_LSE && epi != EPI_HEAD_GRAD;
+  return epi != EPI_POLY && epi != EPI_HILO && epi != EPI_RESID && epi != EPI_ROPE && epi < EPI_HEAD_LSE;
 }
 
 // Limit raise for the configurations of one (layout, epilogue) pair.

@@ -390,7 +390,9 @@ template <int EPI, typename T>
 __device__ inline void epilogue_elem(const GemmProblem& p, const KHead& a, int split,
                                      int row, int col, float v, float v2) {
   if (row >= p.M) return;
-  if constexpr (EPI == EPI_STORE) {
+  if constexpr (EPI == EPI_HEAD_DU) {
+    if (col < p.N) ((T*)p.C[0])[(int64_t)((const int*)p.C[1])[row] * p.ldc + col] = from_f32<T>(v);
+  } else if constexpr (EPI == EPI_STORE) {
     if (col < p.N) {
       const int64_t idx = (int64_t)row * p.ldc + col;
       if (sizeof(T) == 4 || p.splits > 1) ((float*)p.C[0])[(int64_t)split * p.M * p.ldc + idx] = v;
@@ -528,7 +530,9 @@ __device__ inline void epilogue_vec8(const GemmProblem& p, const KHead& a, int s
     return;
   }
   const int64_t idx = (int64_t)row * p.ldc + col0;
-  if constexpr (EPI == EPI_STORE) {
+  if constexpr (EPI == EPI_HEAD_DU) {
+    *(bf16x8s_t*)((__bf16*)p.C[0] + (int64_t)((const int*)p.C[1])[row] * p.ldc + col0) = pack_bf16x8(v);
+  } else if constexpr (EPI == EPI_STORE) {
     *(bf16x8s_t*)((__bf16*)p.C[0] + idx) = pack_bf16x8(v);
   } else if constexpr (EPI == EPI_ATTN_P) {
     const float lse = p.rowvec[row];

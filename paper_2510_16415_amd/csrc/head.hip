@@ -84,10 +84,13 @@ __global__ __launch_bounds__(1024) void head_parts_kernel(const float2* __restri
   if (lse) lse[row] = l;
 }
 
-// out[row, 0 .. cols) = sum of the parts [k][row, col], in their order, V columns per thread.
+// out[row, 0 .. cols) = sum of the parts [k][row, col], in their order, V columns per thread.  list: the rows are *count in
+// number, and row r goes to row list[r].
 template <typename T, int V>
 __global__ __launch_bounds__(256) void head_sum_kernel(const float* __restrict__ part, int parts, int64_t rows, int cols,
-                                                       T* __restrict__ out, int64_t ldo) {
+                                                       T* __restrict__ out, int64_t ldo, const int* __restrict__ list,
+                                                       const int* __restrict__ count) {
+  if (list) rows = *count;
   struct alignas(4 * V) In { float e[V]; };
   struct alignas(sizeof(T) * V) Out { T e[V]; };
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
@@ -103,7 +106,74 @@ __global__ __launch_bounds__(256) void head_sum_kernel(const float* __restrict__
   Out o;
 #pragma unroll
   for (int e = 0; e < V; ++e) o.e[e] = (T)s.e[e];
-  *(Out*)(out + row * ldo + (i - row * cols)) = o;
+  *(Out*)(out + (list ? (int64_t)list[row] : row) * ldo + (i - row * cols)) = o;
+}
+
+// The rows that take part in the gradient, a label in the vocabulary and a dlogp that is not zero, in their order at the front
+// of `list`, the others behind them; *count of the former.  One workgroup, eight rows per thread at a time.
+__global__ __launch_bounds__(1024) void head_list_kernel(const int64_t* __restrict__ labels, const float* __restrict__ dlogp, int rows,
+                                                         int vocab, int* __restrict__ list, int* __restrict__ count) {
+  __shared__ int waves[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int done = 0;      // listed rows of the rounds before
+  for (int base = 0; base < rows; base += 8192) {
+    const int r0 = base + 8 * threadIdx.x;
+    uint32_t on = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (r0 + k < rows) on |= (counted(labels[r0 + k], vocab) && dlogp[r0 + k] != 0.f ? 1u : 0u) << k;
+    const int mine = __popc(on);
+    int before = mine;      // inclusive, over the wave
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int x = __shfl_up(before, o, 64);
+      before += lane >= o ? x : 0;
+    }
+    __syncthreads();        // the round before has read `waves`
+    if (lane == 63) waves[wave] = before;
+    __syncthreads();
+    int at = done + before - mine, all = 0;
+    for (int w = 0; w < 16; ++w) {
+      at += w < wave ? waves[w] : 0;
+      all += waves[w];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int row = r0 + k;
+      if (row >= rows) break;
+      if (on >> k & 1) list[at++] = row;
+      else list[rows - 1 - (row - at)] = row;      // row - at rows in front of this one are not listed
+    }
+    done += all;
+  }
+  if (threadIdx.x == 0) *count = done;
+}
+
+// What the listed rows' gradients are made of, gathered, and zeros for the gradients of the others.  A wave per row.
+struct HeadGather {
+  const __bf16* U; int64_t ldu;
+  const int64_t* labels; const float *lse, *dlogp;
+  const int *list, *count;
+  __bf16* Uc; int64_t* labels_c; float *lse_c, *dlogp_c;
+  __bf16* dU; int64_t lddu;
+  int rows, d;
+};
+__global__ __launch_bounds__(256) void head_gather_kernel(const HeadGather a) {
+  struct alignas(16) V8 { __bf16 e[8]; };
+  const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= a.rows) return;
+  const int src = a.list[r];
+  if (r >= *a.count) {
+    for (int i = lane; i < a.d / 8; i += 64) *(V8*)(a.dU + (int64_t)src * a.lddu + 8 * i) = V8{};
+    return;
+  }
+#pragma unroll 4
+  for (int i = lane; i < a.d / 8; i += 64) *(V8*)(a.Uc + (int64_t)r * a.d + 8 * i) = *(const V8*)(a.U + (int64_t)src * a.ldu + 8 * i);
+  if (lane == 0) {
+    a.labels_c[r] = a.labels[src];
+    a.lse_c[r] = a.lse[src];
+    a.dlogp_c[r] = a.dlogp[src];
+  }
 }
 
 __global__ __launch_bounds__(256) void head_zero_kernel(uint32_t* p, int n) {
@@ -165,9 +235,19 @@ mecefo_status_t check_apart(const void* a, size_t na, const char* an, const void
 constexpr int kMaxParts = 16;
 constexpr int64_t kPartRoom = 32 << 20;      // fp32 elements
 
+// Whether the backward goes by a list of the rows that take part: a list, a copy of their U (0.6 % of the time of 8192 tokens, d 4096,
+// vocabulary 32000) and products over them only.  Which rows these are is known on the device alone.  From about 300 us of
+// products on, where a tenth of the tokens left out is worth more than the two launches; below, and in fp32, all rows.
+bool by_list(const Head& h) {
+  if (!h.bf16) return false;
+  const int forced = options().head_rows.load(std::memory_order_relaxed);
+  return forced ? forced == 2 : 6.0 * h.b * h.dm * h.vocab >= 4e11;
+}
+
 struct HeadWs {
-  size_t U, rstd, Z, zl, dZ, dU, part, dgp, zero, total;
+  size_t U, rstd, Z, zl, dZ, dU, part, dgp, zero, list, count, Uc, labels, lse, dlogp, total;
   int64_t room;
+  bool listed;      // read from the switch once per call
 };
 HeadWs layout(const Head& h, bool backward) {
   HeadWs w;
@@ -176,8 +256,9 @@ HeadWs layout(const Head& h, bool backward) {
   const int64_t act = (int64_t)h.b * h.dm;
   w.U = take(act * h.esz);
   w.rstd = take((int64_t)h.b * 4);
-  w.Z = w.zl = w.dZ = w.dU = w.part = w.dgp = w.zero = off;
+  w.Z = w.zl = w.dZ = w.dU = w.part = w.dgp = w.zero = w.list = w.count = w.Uc = w.labels = w.lse = w.dlogp = off;
   w.room = 0;
+  w.listed = backward && by_list(h);
   if (!backward) {      // bf16: the parts of the log-sum-exps, over 32 columns where the tiles are the smallest; fp32: the products
     w.Z = take(h.bf16 ? ((int64_t)h.vocab + 31) / 32 * h.b * 8 : (int64_t)h.b * h.ldz * 4);
     w.zl = take((int64_t)h.b * 4);
@@ -189,6 +270,14 @@ HeadWs layout(const Head& h, bool backward) {
     w.part = take(w.room * 4);
     w.dgp = take((int64_t)rmsnorm_bwd_blocks(h.b) * h.dm * 4);
     w.zero = take((int64_t)h.dm * h.esz);
+    if (w.listed) {
+      w.list = take((int64_t)h.b * 4);
+      w.count = take(4);
+      w.Uc = take(act * h.esz);
+      w.labels = take((int64_t)h.b * 8);
+      w.lse = take((int64_t)h.b * 4);
+      w.dlogp = take((int64_t)h.b * 4);
+    }
   }
   w.total = off + 256;
   return w;
@@ -304,11 +393,27 @@ mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const vo
   const void* U = X;
   int64_t ldu = desc->ld_act_d;
   void* dZ = base + w.dZ;
+  void* dU = gamma ? base + w.dU : dX;
+  const int64_t lddu = gamma ? h.dm : desc->ld_act_d;
+  const int* list = nullptr;
+  int* count = nullptr;
   if (any) {
     TRY(head_norm(h, w, base, X, gamma, &U, &ldu, s));
+    if (w.listed) {
+      count = (int*)(base + w.count);
+      hipLaunchKernelGGL(head_list_kernel, dim3(1), dim3(1024), 0, s, labels, dlogp, h.b, h.vocab, (int*)(base + w.list), count);
+      HIP_TRY(hipGetLastError());
+      list = (const int*)(base + w.list);
+      const HeadGather a = {(const __bf16*)U, ldu, labels, lse, dlogp, list, count, (__bf16*)(base + w.Uc), (int64_t*)(base + w.labels),
+                            (float*)(base + w.lse), (float*)(base + w.dlogp), (__bf16*)dU, lddu, h.b, h.dm};
+      hipLaunchKernelGGL(head_gather_kernel, dim3(cdiv(h.b, 4)), dim3(256), 0, s, a);
+      HIP_TRY(hipGetLastError());
+      U = a.Uc; ldu = h.dm; labels = a.labels_c; lse = a.lse_c; dlogp = a.dlogp_c;
+    }
     GemmLaunch g = product(h, true, true, EPI_HEAD_GRAD, U, ldu, W, desc->ld_w, dZ, h.ldz, h.b, h.vocab, h.dm);
     GemmProblem& p = g.p[0];
     p.C[1] = const_cast<int64_t*>(labels);
+    p.C[2] = count;
     p.pad_cols = (int)h.ldz;
     p.rowvec = lse;
     p.addend = dlogp;
@@ -316,7 +421,8 @@ mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const vo
     HIP_TRY(launch_gemm(g, s));
   }
   {  // dW = dz^T U   [V x d], contraction over tokens
-    GemmLaunch g = product(h, false, false, EPI_GRAD, dZ, h.ldz, U, ldu, dW, desc->ld_w, h.vocab, h.dm, h.b);
+    GemmLaunch g = product(h, false, false, list ? EPI_HEAD_DW : EPI_GRAD, dZ, h.ldz, U, ldu, dW, desc->ld_w, h.vocab, h.dm, h.b);
+    g.p[0].C[2] = count;
     g.out_f32 = grad_f32;
     g.accumulate = accumulate;
     HIP_TRY(launch_gemm(g, s));
@@ -324,10 +430,10 @@ mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const vo
   int nblk = 0;
   float* dgp = (float*)(base + w.dgp);
   if (any) {  // dU = dz W   [b x d], contraction over the vocabulary
-    void* dU = gamma ? base + w.dU : dX;
-    const int64_t lddu = gamma ? h.dm : desc->ld_act_d;
-    GemmLaunch g = product(h, true, false, EPI_STORE, dZ, h.ldz, W, desc->ld_w, dU, h.dm, h.b, h.dm, h.vocab);
+    GemmLaunch g = product(h, true, false, list ? EPI_HEAD_DU : EPI_STORE, dZ, h.ldz, W, desc->ld_w, dU, h.dm, h.b, h.dm, h.vocab);
     g.p[0].kpad_ok = 1;      // dz has zeros behind the vocabulary
+    g.p[0].C[1] = const_cast<int*>(list);
+    g.p[0].C[2] = count;
     if (h.bf16) bf16_plan_splits(g, w.room);
     else f32_plan_splits(g, (int)(w.room / ((int64_t)h.b * h.dm)));
     const int parts = g.p[0].splits;
@@ -340,7 +446,7 @@ mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const vo
       auto sum = [&](auto type, auto v) {      // bf16 rows are whole vectors of eight
         using T = decltype(type);
         constexpr int V = decltype(v)::value;
-        hipLaunchKernelGGL((head_sum_kernel<T, V>), dim3((unsigned)((n / V + 255) / 256)), dim3(256), 0, s, part, parts, (int64_t)h.b, h.dm, (T*)dU, lddu);
+        hipLaunchKernelGGL((head_sum_kernel<T, V>), dim3((unsigned)((n / V + 255) / 256)), dim3(256), 0, s, part, parts, (int64_t)h.b, h.dm, (T*)dU, lddu, list, count);
       };
       if (h.bf16) sum(__bf16{}, std::integral_constant<int, 4>{});
       else if (h.dm % 4 == 0 && lddu % 4 == 0 && (uintptr_t)dU % 16 == 0) sum(float{}, std::integral_constant<int, 4>{});

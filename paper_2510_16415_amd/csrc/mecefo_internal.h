@@ -23,6 +23,10 @@ enum Epilogue : int {
                        // over part_cols columns and the sum of 2^(z' - that); C2 (fp32) [row] = z at the row's label, C1 (int64)   (bf16, NT)
   EPI_HEAD_GRAD = 12,  // C0[row, col] = scale * addend[row] * ([col = label] - exp(scale * acc - rowvec[row])), 0 where the label C1[row]
                        // (int64) is no column; columns [N, pad_cols) are set to zero   (NT)
+  EPI_HEAD_DU = 13,    // EPI_STORE whose row r is row C1[r] (int32) of C0; cut along K: [split][rows x ldc] in order   (bf16, NN)
+  EPI_HEAD_DW = 14,    // EPI_GRAD   (bf16, TN)
+                       // EPI_HEAD_GRAD, _DU and _DW: C2, where it is given, is the address of an int that M (_DW: K) is if that is less:
+                       // how many of the rows there are is known on the device only
 };
 
 constexpr int kMaxProblems = 4;   // of one launch
@@ -129,6 +133,7 @@ inline const char* const kTileOptionName[kTileOptions] = {"auto", "S", "L4", "L8
 struct Options {
   std::atomic<int> tile{0};        // bf16 GEMM configuration, index into kTileOptionName
   std::atomic<int> attn_gemm{0};   // 1: attention through batched GEMM launches instead of the fused kernels
+  std::atomic<int> head_rows{0};   // head backward: 1 all rows, 2 the scored ones
 };
 Options& options();
 

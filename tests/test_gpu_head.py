@@ -211,3 +211,112 @@ def test_repeats_are_bit_equal_and_streams_do_not_mix():
     assert all(torch.equal(a, b) for g in got for a, b in zip(g, first))
     again = run_bwd(X, W, labels, first[1], c, "bf16")
     assert all(np.array_equal(a, b) for a, b in zip(grads[:2], again[:2]))
+
+
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("skip", [0.0, 0.3, 0.9, 1.0])
+@pytest.mark.parametrize("b,d,v", [(1, 16, 9), (5, 40, 33), (64, 128, 257), (257, 64, 1000), (700, 256, 515), (8300, 16, 40)])
+def test_backward_by_the_list_of_scored_rows(b, d, v, skip, grad, mecefo_option):
+    X, W, labels, c = case(b, d, v, "bf16", seed=8, skip=skip)
+    c[::7] = 0.0      # a label, and no gradient
+    mecefo_option("head", "scored")
+    _, L = run_fwd(X, W, labels, "bf16", pad=8)
+    out = ((labels < 0) | (labels >= v)) | (c == 0)
+    dX, dW, _ = run_bwd(X, W, labels, L, c, "bf16", pad=8, grad=grad)
+    wX, wW = T.head_bwd(X, W, labels, c)
+    assert not dX[out].any()
+    assert relerr(dX, wX) <= GATE["bf16"] and relerr(dW, wW) <= GATE["bf16"]
+    over, more = dW, run_bwd(X, W, labels, L, c, "bf16", pad=8, grad=grad, accumulate=1)[1]
+    step = 2.0 ** -8 if grad == "bf16" else U32
+    assert (np.abs(more - (over + 0.25)) <= step * (np.abs(over) + np.abs(more) + 0.25)).all()
+
+
+@pytest.mark.parametrize("tile", ["S", "S4", "T", "T2", "X", "L8", "LT", "K"])
+@pytest.mark.parametrize("b,d,v", [(333, 192, 1111), (600, 512, 700)])
+def test_the_list_on_every_tile(tile, b, d, v, mecefo_option):
+    X, W, labels, c = case(b, d, v, "bf16", seed=9, skip=0.4)
+    mecefo_option("head", "scored")
+    mecefo_option("tile", tile)
+    _, L = run_fwd(X, W, labels, "bf16")
+    dX, dW, _ = run_bwd(X, W, labels, L, c, "bf16")
+    wX, wW = T.head_bwd(X, W, labels, c)
+    assert relerr(dX, wX) <= GATE["bf16"] and relerr(dW, wW) <= GATE["bf16"]
+
+
+def test_the_list_with_a_norm_and_with_few_long_products(mecefo_option):
+    mecefo_option("head", "scored")
+    for b, d, v in ((300, 64, 20000), (40, 2048, 4000)):      # dU cut along the vocabulary
+        X, W, labels, c = case(b, d, v, "bf16", seed=10, skip=0.5, std=d ** -0.5)
+        gamma = I.round_to_bf16_grid(1 + 0.2 * np.random.default_rng(4).standard_normal(d))
+        x = X.astype(np.float64)
+        rs = 1 / np.sqrt((x * x).mean(axis=1, keepdims=True) + float(np.float32(1e-6)))
+        N = x * rs
+        U = I.round_to_bf16_grid(N * gamma).astype(np.float64)
+        _, L = run_fwd(X, W, labels, "bf16", gamma=gamma)
+        dX, dW, dg = run_bwd(X, W, labels, L, c, "bf16", gamma=gamma)
+        dU, wW = T.head_bwd(U, W, labels, c)
+        dN = dU * gamma
+        gate = 4 * 2.0 ** -8      # as with a norm above
+        assert relerr(dX, rs * (dN - N * (dN * N).mean(axis=1, keepdims=True))) <= gate
+        assert relerr(dW, wW) <= gate and relerr(dg, (dU * N).sum(axis=0)) <= gate
+
+
+def test_large_backwards_go_by_the_list_on_their_own(mecefo_option):
+    """The rule's two sides on one size: the same gradients, and the workspace of the side that is taken."""
+    b, d, v = 1024, 1024, 65600      # 4.1e11 operations
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    X, W = ((torch.randn(s, device="cuda", generator=gen) * k).bfloat16() for s, k in (((b, d), 1.0), ((v, d), 0.02)))
+    labels = torch.randint(-v // 4, v, (b,), device="cuda", generator=gen)
+    c = torch.randn(b, device="cuda", generator=gen)
+    desc = B.make_head_desc(b, d, v, B.BF16, B.BF16)
+    logp, L = torch.empty(b, device="cuda"), torch.empty(b, device="cuda")
+    B.mecefo_head_logprob_fwd(desc, X, None, W, labels, logp, L, poisoned_ws(B.mecefo_head_workspace_bytes(desc, False)))
+    got, need = {}, {}
+    for rows in ("all", "scored", "auto"):
+        mecefo_option("head", rows)
+        need[rows] = B.mecefo_head_workspace_bytes(desc, True)
+        dX, dW = torch.empty_like(X), torch.empty_like(W)
+        B.mecefo_head_logprob_bwd(desc, X, None, W, labels, L, c, dX, None, dW, 0, poisoned_ws(need[rows]))
+        got[rows] = (dX.float(), dW.float())
+    assert need["auto"] == need["scored"] > need["all"]
+    z = X.double() @ W.double().t()
+    p = torch.exp(z - torch.logsumexp(z, 1, keepdim=True)).neg_()
+    on = labels >= 0
+    p[torch.arange(b, device="cuda"), labels.clamp(min=0)] += on.double()
+    p *= (c.double() * on)[:, None]
+    for dX, dW in got.values():
+        for x, y in ((dX, p @ W.double()), (dW, p.t() @ X.double())):
+            assert float((x.double() - y).norm() / y.norm()) <= GATE["bf16"]
+    assert all(torch.equal(a, s) for a, s in zip(got["auto"], got["scored"]))
+
+
+def test_a_graph_follows_the_labels_of_its_replays(mecefo_option):
+    B.mecefo_init()
+    mecefo_option("head", "scored")
+    b, d, v = 300, 128, 700
+    X, W, labels, c = case(b, d, v, "bf16", seed=11, skip=0.0)
+    desc = B.make_head_desc(b, d, v, B.BF16)
+    t = dict(X=dev(X, "bf16"), W=dev(W, "bf16"), labels=torch.from_numpy(labels).cuda(), c=torch.from_numpy(c).cuda(),
+             logp=torch.empty(b, device="cuda"), L=torch.empty(b, device="cuda"), dX=torch.empty(b, d, dtype=torch.bfloat16, device="cuda"),
+             dW=torch.empty(v, d, device="cuda"))
+    ws = [poisoned_ws(B.mecefo_head_workspace_bytes(desc, k)) for k in (False, True)]
+
+    def run():
+        s = torch.cuda.current_stream()
+        B.mecefo_head_logprob_fwd(desc, t["X"], None, t["W"], t["labels"], t["logp"], t["L"], ws[0], s)
+        B.mecefo_head_logprob_bwd(desc, t["X"], None, t["W"], t["labels"], t["L"], t["c"], t["dX"], None, t["dW"], 0, ws[1], s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    rng = np.random.default_rng(12)
+    for share in (0.0, 0.5, 1.0, 0.97, 0.1):
+        now = np.where(rng.random(b) < share, -1, labels)
+        t["labels"].copy_(torch.from_numpy(now))
+        graph.replay()
+        torch.cuda.synchronize()
+        wX, wW = T.head_bwd(X, W, now, c)
+        assert relerr(t["dX"].float().cpu().numpy(), wX) <= GATE["bf16"] and relerr(t["dW"].cpu().numpy(), wW) <= GATE["bf16"]
+        got = [x.clone() for x in (t["dX"], t["dW"])]
+        run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, x) for a, x in zip(got, (t["dX"], t["dW"])))

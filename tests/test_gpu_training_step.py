@@ -196,7 +196,9 @@ def test_two_graphs_with_workspaces_of_their_own_may_overlap():
 
 @pytest.mark.parametrize("b,d,v", [(1, 64, 7), (77, 128, 1001), (600, 64, 515)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_head_stays_inside_its_workspace(b, d, v, dtype):
+@pytest.mark.parametrize("rows", ["all", "scored"])
+def test_head_stays_inside_its_workspace(b, d, v, dtype, rows, mecefo_option):
+    mecefo_option("head", rows)
     tt, code = (torch.bfloat16, B.BF16) if dtype == "bf16" else (torch.float32, B.F32)
     X, W, gamma = (torch.randn(s, device="cuda").to(tt) for s in ((b, d), (v, d), (d,)))
     labels, logp, lse = torch.randint(0, v, (b,), device="cuda"), torch.empty(b, device="cuda"), torch.empty(b, device="cuda")

@@ -224,3 +224,17 @@ def test_ranges_of_sequences_and_slices(tmp_path):
     exe = tmp_path / "loss_ranges"
     subprocess.run(["g++", "-std=c++17", "-Wall", os.path.join(here, "loss_ranges.cpp"), "-o", str(exe)], check=True)
     assert subprocess.run([str(exe)], capture_output=True, text=True).stdout == "ok\n"
+
+
+def test_head_option():
+    refused(INV, "option head", B.mecefo_set_option, "head", "some")
+    h = head(tokens=4096, d_model=1024, vocab=32000)
+    need = {}
+    try:
+        for v in ("all", "scored", "auto"):
+            B.mecefo_set_option("head", v)
+            need[v] = B.mecefo_head_workspace_bytes(h, True), B.mecefo_head_workspace_bytes(head(), True), B.mecefo_head_workspace_bytes(h, False)
+    finally:
+        B.mecefo_set_option("head", "auto")
+    assert need["auto"][0] == need["scored"][0] >= need["all"][0] + 4096 * (1024 * 2 + 20) and need["auto"][1] == need["all"][1] < need["scored"][1]
+    assert len({n[2] for n in need.values()}) == 1
