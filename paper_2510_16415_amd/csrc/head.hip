@@ -235,13 +235,15 @@ mecefo_status_t check_apart(const void* a, size_t na, const char* an, const void
 constexpr int kMaxParts = 16;
 constexpr int64_t kPartRoom = 32 << 20;      // fp32 elements
 
-// Whether the backward goes by a list of the rows that take part: a list, a copy of their U (0.6 % of the time of 8192 tokens, d 4096,
-// vocabulary 32000) and products over them only.  Which rows these are is known on the device alone.  From about 300 us of
-// products on, where a tenth of the tokens left out is worth more than the two launches; below, and in fp32, all rows.
+// Whether the backward goes by a list of the rows that take part: a list, a copy of their U and products over them only.  Which
+// rows these are is known on the device alone; two launches and the copy cost 10 to 20 us, which is 0.4 % of the largest calls.  All rows /
+// the list, us, with none, a tenth and three tenths of the tokens out: [8192 x 4096], vocabulary 32000, 5240 / 5259, 5211 / 4966,
+// 5151 / 4237; [2048 x 2048] 735 / 735, 730 / 701, 720 / 579; [1024 x 1024] (2e11 operations) 232 / 231, 219 / 222, 219 / 194; [512 x 2048]
+// 227 / 236, 225 / 228, 223 / 213; [1024 x 512] (1e11) 140 / 150, 140 / 146, 140 / 133.  In fp32 all rows.
 bool by_list(const Head& h) {
   if (!h.bf16) return false;
   const int forced = options().head_rows.load(std::memory_order_relaxed);
-  return forced ? forced == 2 : 6.0 * h.b * h.dm * h.vocab >= 4e11;
+  return forced ? forced == 2 : 6.0 * h.b * h.dm * h.vocab >= 2e11;
 }
 
 struct HeadWs {
