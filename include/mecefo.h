@@ -14,6 +14,8 @@
  * Around that hot path, further below: the standard-mode backward (Alg. 3, first branch), the
  * block forward of both modes (Alg. 2), a stack of blocks in neighbor mode, tunable variants,
  * the projection refresh (Alg. 3, every tau steps), Eq. (1) gradient averaging and AdamW (Alg. 1).
+ * And what lies between a stack's output and the gradient that it takes back: the LM head's log-probabilities, a preference
+ * and a policy loss; and 8-bit checkpoints of the stored tensors.
  *
  * Notation (row-major, token index along rows, weights in [out x in] layout):
  *   b tokens, d = d_model, f = d_ff, r = rank.
