@@ -414,7 +414,8 @@ mecefo_status_t mecefo_stack_bwd_skip_ckpt(const mecefo_ffn_desc_t* desc, int n_
  * The logits are never stored by the forward.  dtype MECEFO_BF16: products accumulated in fp32, exponentials and their
  * sums in fp32; with gamma, U is rounded to bf16.  d_model must be a multiple of 8, vocab may be any size.
  * The backward forms the products again and stores dz_iv = logit_scale * dlogp_i * ([v = labels[i]] - exp(z_iv - lse_i)) in
- * dtype (b * up8(vocab) elements of the workspace, which must stay below 2 GiB: split the token batch and accumulate);
+ * dtype (b * up8(vocab) elements of the workspace, which must stay below 2 GiB, as must X and W: split the token batch and
+ * accumulate; so must the products that the fp32 forward stores, and the bf16 forward's b * ceil(vocab / 32) parts of 8 bytes);
  *   dU = dz W;  dX = dU through the norm's backward, or dU;  dW = dz^T U and dgamma in grad_dtype, overwritten or added to. */
 typedef struct {
   int64_t tokens;               /* b */
@@ -441,7 +442,7 @@ mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const vo
  * [offsets[k], offsets[k + 1]) of the token arrays (offsets: device memory, not decreasing, within [0, tokens]; a sequence may
  * be empty; offsets that break this give undefined results, but nothing outside the arrays is touched).  mask [tokens]: a token
  * with 0 is not counted, and what the arrays hold for it is not used; NULL counts all.  dlogp [tokens] is written
- * as a whole: zero for what is not counted or belongs to no sequence.  Sums are taken in fp64, in an order that depends on
+ * as a whole: zero for what is not counted or belongs to no sequence; no output may overlap an input.  Sums are taken in fp64, in an order that depends on
  * the sizes only.  All values fp32, at most 2^20 sequences. */
 
 /* Preference loss over pairs; sequence 2i is the preferred answer of pair i, sequence 2i + 1 the other one.

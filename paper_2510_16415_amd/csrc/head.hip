@@ -194,7 +194,9 @@ struct Head {
 #define TRY(x) do { mecefo_status_t st__ = (x); if (st__ != MECEFO_OK) return st__; } while (0)
 #define HIP_TRY(x) do { hipError_t e__ = (x); if (e__ != hipSuccess) return FAIL(MECEFO_ERR_LAUNCH, "%s: %s", #x, hipGetErrorString(e__)); } while (0)
 
-mecefo_status_t check_desc(const mecefo_head_desc_t* d, Head* h) {
+// The products read their operands with 32-bit offsets: X, W and the backward's dz stay below 2 GiB; outputs are addressed with 64
+// bits.  The bf16 forward stores no logits: its parts at their smallest tiles, 8 bytes to 32 columns, are what is bounded then.
+mecefo_status_t check_desc(const mecefo_head_desc_t* d, bool backward, Head* h) {
   if (!d) return FAIL(MECEFO_ERR_INVALID_ARG, "descriptor is NULL");
   if (d->dtype != MECEFO_F32 && d->dtype != MECEFO_BF16) return FAIL(MECEFO_ERR_INVALID_ARG, "dtype must be MECEFO_F32 or MECEFO_BF16");
   if (d->grad_dtype != MECEFO_F32 && d->grad_dtype != d->dtype) return FAIL(MECEFO_ERR_UNSUPPORTED, "grad_dtype must be MECEFO_F32 or equal to dtype");
@@ -206,7 +208,9 @@ mecefo_status_t check_desc(const mecefo_head_desc_t* d, Head* h) {
   h->esz = h->bf16 ? 2 : 4;
   if (h->bf16 && d->d_model % 8) return FAIL(MECEFO_ERR_UNSUPPORTED, "bf16 path needs d_model to be a multiple of 8 (got %d)", d->d_model);
   if (h->bf16 && (d->ld_act_d % 8 || d->ld_w % 8)) return FAIL(MECEFO_ERR_INVALID_ARG, "bf16 path needs every row stride to be a multiple of 8 elements");
-  if (reaches_2gib(d->tokens, d->ld_act_d, h->esz) || reaches_2gib(d->vocab, d->ld_w, 4) || reaches_2gib(d->tokens, up(d->vocab, 8), h->esz))
+  const bool parts = h->bf16 && !backward;
+  if (reaches_2gib(d->tokens, d->ld_act_d, h->esz) || reaches_2gib(d->vocab, d->ld_w, h->esz) ||
+      reaches_2gib(d->tokens, parts ? ((int64_t)d->vocab + 31) / 32 : up(d->vocab, 8), parts ? 8 : h->esz))
     return FAIL(MECEFO_ERR_UNSUPPORTED, "a tensor reaches 2 GiB; split the token batch");
   h->b = (int)d->tokens;
   h->dm = d->d_model;
@@ -331,7 +335,7 @@ extern "C" {
 
 mecefo_status_t mecefo_head_workspace_bytes(const mecefo_head_desc_t* desc, int backward, size_t* out_bytes) {
   Head h;
-  TRY(check_desc(desc, &h));
+  TRY(check_desc(desc, backward != 0, &h));
   if (!out_bytes) return FAIL(MECEFO_ERR_INVALID_ARG, "out_bytes is NULL");
   *out_bytes = layout(h, backward != 0).total;
   return MECEFO_OK;
@@ -341,7 +345,7 @@ mecefo_status_t mecefo_head_logprob_fwd(const mecefo_head_desc_t* desc, const vo
                                         const int64_t* labels, float* logp, float* lse, void* ws, size_t ws_bytes,
                                         void* hip_stream) {
   Head h;
-  TRY(check_desc(desc, &h));
+  TRY(check_desc(desc, false, &h));
   const bool any = h.b > 0;
   TRY(check_ptr(h, X, "X", any)); TRY(check_ptr(h, gamma, "gamma", false)); TRY(check_ptr(h, W, "W", true));
   TRY(check_small(labels, "labels", 8, any)); TRY(check_small(logp, "logp", 4, any)); TRY(check_small(lse, "lse", 4, false));
@@ -378,7 +382,7 @@ mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const vo
                                         const int64_t* labels, const float* lse, const float* dlogp, void* dX, void* dgamma,
                                         void* dW, int accumulate, void* ws, size_t ws_bytes, void* hip_stream) {
   Head h;
-  TRY(check_desc(desc, &h));
+  TRY(check_desc(desc, true, &h));
   const bool any = h.b > 0, grad_f32 = desc->grad_dtype == MECEFO_F32;
   TRY(check_ptr(h, X, "X", any)); TRY(check_ptr(h, gamma, "gamma", false)); TRY(check_ptr(h, W, "W", true));
   TRY(check_small(labels, "labels", 8, any)); TRY(check_small(lse, "lse", 4, any)); TRY(check_small(dlogp, "dlogp", 4, any));

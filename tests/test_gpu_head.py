@@ -320,3 +320,52 @@ def test_a_graph_follows_the_labels_of_its_replays(mecefo_option):
         run()
         torch.cuda.synchronize()
         assert all(torch.equal(a, x) for a, x in zip(got, (t["dX"], t["dW"])))
+
+
+def test_forward_of_more_logits_than_2_gib():
+    """b V logits of 2.3 GB that are not stored; a sample of the rows, the last ones among them."""
+    b, d, v = 16411, 64, 70003
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    X = torch.randn(b, d, device="cuda", generator=gen).bfloat16()
+    W = (torch.randn(v, d, device="cuda", generator=gen) * 0.2).bfloat16()
+    labels = torch.randint(0, v, (b,), device="cuda", generator=gen)
+    labels[-1] = v - 1
+    desc = B.make_head_desc(b, d, v, B.BF16, B.F32)
+    logp, L = torch.full((b,), 9.0, device="cuda"), torch.full((b,), 9.0, device="cuda")
+    B.mecefo_head_logprob_fwd(desc, X, None, W, labels, logp, L, poisoned_ws(B.mecefo_head_workspace_bytes(desc, False)))
+    rows = torch.cat([torch.arange(0, b, 797), torch.arange(b - 20, b)])
+    x, w = (t.float().cpu().numpy() for t in (X[rows.cuda()], W))
+    want, lse = T.head_fwd(x, w, labels.cpu()[rows].numpy())
+    tol = logp_bound(x, w, 1.0, v)
+    assert (np.abs(logp.cpu()[rows].numpy() - want) <= tol).all() and (np.abs(L.cpu()[rows].numpy() - lse) <= tol).all()
+
+
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_weight_gradient_beyond_2_gib(accumulate):
+    """An fp32 dW of 2.2 GB: rows at both ends, and around 2 GiB."""
+    b, d, v = 96, 512, 1060003
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    X = torch.randn(b, d, device="cuda", generator=gen).bfloat16()
+    W = (torch.randn(v, d, device="cuda", generator=gen) * 0.1).bfloat16()
+    at = (1 << 31) // (4 * d)
+    rows = torch.cat([torch.arange(0, 40), torch.arange(at - 40, at + 40), torch.arange(v - 40, v)]).cuda()
+    labels = rows[torch.randint(0, len(rows), (b,), device="cuda", generator=gen)]
+    labels[-1] = v - 1
+    c = torch.randn(b, device="cuda", generator=gen)
+    desc = B.make_head_desc(b, d, v, B.BF16, B.F32)
+    z = torch.cat([X.double() @ W[i:i + 65536].double().T for i in range(0, v, 65536)], 1)
+    lse = torch.logsumexp(z, 1)
+    dz = -torch.exp(z - lse[:, None])
+    dz[torch.arange(b), labels] += 1.0
+    dz *= c.double()[:, None]
+    dX, dW = torch.full((b, d), 5.0, device="cuda").bfloat16(), torch.full((v, d), 0.25, device="cuda")
+    B.mecefo_head_logprob_bwd(desc, X, None, W, labels, lse.float(), c, dX, None, dW, accumulate,
+                              poisoned_ws(B.mecefo_head_workspace_bytes(desc, True)))
+    want = dz[:, rows].T @ X.double()
+    got = dW[rows].double() - (0.25 if accumulate else 0.0)
+    # 0.25 + the gradient is rounded to fp32 where it is added to
+    assert (got - want).norm() <= GATE["bf16"] * want.norm() + accumulate * U32 * (0.25 + want.abs().max()) * want.numel() ** 0.5
+    wx = torch.zeros(b, d, dtype=torch.float64, device="cuda")
+    for i in range(0, v, 65536):
+        wx += dz[:, i:i + 65536] @ W[i:i + 65536].double()
+    assert (dX.double() - wx).norm() <= GATE["bf16"] * wx.norm()

@@ -90,9 +90,30 @@ def test_head_descriptor_refusals(desc, status, text):
     refused(status, text, B.mecefo_head_logprob_fwd, head(**desc), at(), None, at(), at(), at(), at(), at(), STREAM)
 
 
+@pytest.mark.parametrize("dtype,tokens,d_model,vocab,forward,backward", [
+    (B.BF16, 16384, 64, 65536, True, False),          # dz of 2 GiB
+    (B.BF16, 16384, 64, 65528, True, True),
+    (B.BF16, 131072, 64, 65536, False, False),        # the forward's parts too
+    (B.BF16, 131071, 64, 65536, True, False),
+    (B.F32, 16384, 64, 32768, False, False),
+    (B.F32, 16384, 64, 32760, True, True),
+    (B.BF16, 64, 4096, 262143, True, True),           # W below 2 GiB, an fp32 dW above
+    (B.BF16, 64, 4096, 262144, False, False),
+    (B.F32, 64, 4096, 131071, True, True),
+    (B.F32, 64, 4096, 131072, False, False),
+])
+def test_head_sizes_at_their_limits(dtype, tokens, d_model, vocab, forward, backward):
+    h = head(dtype=dtype, tokens=tokens, d_model=d_model, vocab=vocab)
+    for back, allowed in ((False, forward), (True, backward)):
+        if allowed:
+            assert B.mecefo_head_workspace_bytes(h, back) > 0
+        else:
+            refused(UNS, "2 GiB", B.mecefo_head_workspace_bytes, h, back)
+
+
 def head_args(h, **change):
     """Places for every argument of the backward, apart from each other."""
-    a = dict(X=at(256), gamma=at(1024), W=at(2048), labels=at(3072), lse=at(3200), dlogp=at(3300), dX=at(3584),
+    a = dict(X=at(256), gamma=at(1024), W=at(2048), labels=at(2976), lse=at(3200), dlogp=at(3300), dX=at(3584),
              dgamma=at(4096), dW=at(5120), ws=at(8192))
     a.update(change)
     return a
@@ -101,7 +122,7 @@ def head_args(h, **change):
 @pytest.mark.parametrize("change,status,text", [
     (dict(X=None), INV, "X is NULL"), (dict(W=None), INV, "W is NULL"), (dict(labels=None), INV, "labels is NULL"),
     (dict(X=at(264)), INV, "X is not 16-byte"), (dict(gamma=at(1028)), INV, "gamma is not"), (dict(W=at(2056)), INV, "W is not"),
-    (dict(labels=at(3076)), INV, "labels is not 8-byte"), (dict(lse=at(3201)), INV, "lse is not 4-byte"),
+    (dict(labels=at(2980)), INV, "labels is not 8-byte"), (dict(lse=at(3201)), INV, "lse is not 4-byte"),
     (dict(ws=None), WS, "needed"), (dict(ws=at(8192)[:64]), WS, "needed"),
 ])
 def test_head_pointer_refusals(change, status, text):
