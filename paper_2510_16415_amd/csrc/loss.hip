@@ -26,6 +26,8 @@ constexpr int kWaveSlices = 16;      // from here on a wave adds up a sequence's
 // them: preference 2 x 20 to 16 x 32 7.6 to 8.1 / 11.4, policy 8.0 to 10 / 11.5.
 constexpr int kSmallTokens = 512, kSmallSeqs = 16;
 
+constexpr int kClearTokens = 16384;
+
 struct Part { double sum; double count; };
 
 __device__ inline TokenRange sequence(const int64_t* offsets, int64_t tokens, int k) { return token_range(offsets[k], offsets[k + 1], tokens); }
@@ -141,15 +143,16 @@ __global__ __launch_bounds__(kThreads) void preference_sums_kernel(const PrefArg
   if (threadIdx.x == 0) a.parts[blockIdx.x] = Part{v[0], v[1]};
 }
 
-// Zeros for the tokens in front of the first sequence and behind the last one.
-__device__ inline void clear_outside(const int64_t* offsets, int64_t tokens, int n, float* dlogp) {
+// Zeros for the tokens in front of the first sequence and behind the last one, workgroup `at` of `of`.
+__device__ inline void clear_outside(const int64_t* offsets, int64_t tokens, int n, float* dlogp, int at, int of) {
   const int64_t first = n > 0 ? sequence(offsets, tokens, 0).lo : tokens, last = n > 0 ? sequence(offsets, tokens, n - 1).hi : tokens;
-  for (int64_t t = threadIdx.x; t < first; t += blockDim.x) dlogp[t] = 0.f;
-  for (int64_t t = last + threadIdx.x; t < tokens; t += blockDim.x) dlogp[t] = 0.f;
+  const int64_t t0 = (int64_t)at * blockDim.x + threadIdx.x, stride = (int64_t)of * blockDim.x;
+  for (int64_t t = t0; t < first; t += stride) dlogp[t] = 0.f;
+  for (int64_t t = last + t0; t < tokens; t += stride) dlogp[t] = 0.f;
 }
 
 // Workgroups 0 .. 2 * pairs * slices - 1: the gradients of a slice; the one behind them: the mean loss, every pair's margin and
-// rewards, and the tokens of no sequence.  It takes a wave to a pair where sequences have many slices, else a thread (64 pairs
+// rewards; the last ones: the tokens of no sequence.  The one takes a wave to a pair where sequences have many slices, else a thread (64 pairs
 // of 4 slices: the launch 28 us with a wave to a pair, 6 with a thread).
 __global__ __launch_bounds__(kThreads) void preference_grad_kernel(const PrefArgs a) {
   const int grads = 2 * a.pairs * a.slices;
@@ -175,9 +178,9 @@ __global__ __launch_bounds__(kThreads) void preference_grad_kernel(const PrefArg
     }
     total = block_sum(total);
     if (threadIdx.x == 0) a.loss[0] = a.pairs > 0 ? (float)(total / a.pairs) : 0.f;
-    clear_outside(a.offsets, a.tokens, 2 * a.pairs, a.dlogp);
     return;
   }
+  if ((int)blockIdx.x > grads) return clear_outside(a.offsets, a.tokens, 2 * a.pairs, a.dlogp, blockIdx.x - grads - 1, gridDim.x - grads - 1);
   const int k = blockIdx.x / a.slices, j = blockIdx.x - k * a.slices;
   const TokenRange r = token_slice(sequence(a.offsets, a.tokens, k), j, a.slices);
   write_gradients(a, r, threadIdx.x, kThreads, [&]() {
@@ -216,7 +219,7 @@ __global__ __launch_bounds__(1024) void preference_small_kernel(const PrefArgs a
   total = block_sum(total);      // and its barriers: the slopes are written
   if (threadIdx.x == 0) a.loss[0] = a.pairs > 0 ? (float)(total / a.pairs) : 0.f;
   for (int k = wave; k < 2 * a.pairs; k += 16) write_gradients(a, sequence(a.offsets, a.tokens, k), lane, 64, [&]() { return slope[k]; });
-  clear_outside(a.offsets, a.tokens, 2 * a.pairs, a.dlogp);
+  clear_outside(a.offsets, a.tokens, 2 * a.pairs, a.dlogp, 0, 1);
 }
 
 struct PolicySums { double loss, kl, clipped; uint32_t count; };      // without the tokens' weights
@@ -317,9 +320,10 @@ __global__ __launch_bounds__(kThreads) void policy_tokens_kernel(const PolicyArg
   a.counts[blockIdx.x] = (uint32_t)t[3];
 }
 
-// Workgroup seqs * slices: the results, and the tokens of no sequence.
+// Workgroup seqs * slices: the results; those behind it: the tokens of no sequence.
 __global__ __launch_bounds__(kThreads) void policy_scale_kernel(const PolicyArgs a) {
   const int grads = a.seqs * a.slices, k = blockIdx.x / a.slices, j = blockIdx.x - k * a.slices, lane = threadIdx.x & 63;
+  if ((int)blockIdx.x > grads) return clear_outside(a.offsets, a.tokens, a.seqs, a.dlogp, blockIdx.x - grads - 1, gridDim.x - grads - 1);
   const bool total = (int)blockIdx.x == grads, waves = a.slices >= kWaveSlices;
   auto wave_count = [&](int i) {
     double c = 0.0;
@@ -371,7 +375,6 @@ __global__ __launch_bounds__(kThreads) void policy_scale_kernel(const PolicyArgs
   }
   block_sums(t);
   if (threadIdx.x == 0) policy_results(a, t[0], t[1], t[2]);
-  clear_outside(a.offsets, a.tokens, a.seqs, a.dlogp);
 }
 
 // A small batch in one workgroup and one launch: a wave to a sequence.
@@ -394,7 +397,7 @@ __global__ __launch_bounds__(1024) void policy_small_kernel(const PolicyArgs a) 
     scale_gradients(a, sequence(a.offsets, a.tokens, k), lane, 64, [&]() { return (float)w; });
     if (lane == 0) { t[0] += sums[k].loss * w; t[1] += sums[k].kl * w; t[2] += sums[k].clipped * w; }
   }
-  clear_outside(a.offsets, a.tokens, a.seqs, a.dlogp);
+  clear_outside(a.offsets, a.tokens, a.seqs, a.dlogp, 0, 1);
   block_sums(t);
   if (threadIdx.x == 0) policy_results(a, t[0], t[1], t[2]);
 }
@@ -407,6 +410,9 @@ int slices_of(int64_t tokens, int64_t sequences) {
   const int64_t least = tokens / (4 * kCUs), size = least > kSliceTokens ? least : kSliceTokens, n = (mean + size - 1) / size;
   return (int)(n < 1 ? 1 : n > kMaxSlices ? kMaxSlices : n);
 }
+
+// Workgroups that clear the tokens of no sequence: how many those are only the device knows.
+int clears(int64_t tokens) { return (int)(tokens / kClearTokens) + 1; }
 
 mecefo_status_t check_sizes(int64_t tokens, int64_t sequences) {
   if (tokens < 0 || sequences < 0) return (mecefo_status_t)fail(MECEFO_ERR_INVALID_ARG, "tokens and the number of sequences must be >= 0");
@@ -488,7 +494,7 @@ mecefo_status_t mecefo_preference_loss(const mecefo_preference_desc_t* desc, con
     hipLaunchKernelGGL(preference_sums_kernel, dim3(grads), dim3(kThreads), 0, s, a);
     LAUNCHED("preference_loss");
   }
-  hipLaunchKernelGGL(preference_grad_kernel, dim3(grads + 1), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(preference_grad_kernel, dim3(grads + 1 + clears(desc->tokens)), dim3(kThreads), 0, s, a);
   LAUNCHED("preference_loss");
   return MECEFO_OK;
 }
@@ -527,7 +533,7 @@ mecefo_status_t mecefo_policy_loss(const mecefo_policy_desc_t* desc, const float
     hipLaunchKernelGGL(policy_tokens_kernel, dim3(grads), dim3(kThreads), 0, s, a);
     LAUNCHED("policy_loss");
   }
-  hipLaunchKernelGGL(policy_scale_kernel, dim3(grads + 1), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(policy_scale_kernel, dim3(grads + 1 + clears(desc->tokens)), dim3(kThreads), 0, s, a);
   LAUNCHED("policy_loss");
   return MECEFO_OK;
 }

@@ -193,3 +193,20 @@ def test_repeats_are_bit_equal_on_other_streams():
     adv = rng.standard_normal(40).astype(np.float32)
     a, b = (run_policy(lp, old, ref, adv, mask, off, kl=0.1, by_seq=True) for _ in range(2))
     assert all(np.array_equal(a[k], b[k]) for k in a)
+
+
+@pytest.mark.parametrize("front,used,behind", [(70001, 900, 60002), (0, 3, 200000), (131073, 0, 0)])
+def test_tokens_of_no_sequence_get_zeros(front, used, behind):
+    """A buffer that is larger than the batch in it: what lies outside holds NaN and is not looked at."""
+    rng = np.random.default_rng([front, used])
+    n = front + used + behind
+    off = front + np.array([0, used // 3, used // 2, used // 2, used], np.int64)
+    inside = np.zeros(n, bool)
+    inside[front:front + used] = True
+    lp, old, r, _ = arrays(rng, n, 0.0)
+    adv = rng.standard_normal(n).astype(np.float32)
+    bad = [np.where(inside, x, np.float32(np.nan)) for x in (lp, r, old, adv)]
+    check_preference(run_preference(bad[0], bad[1], None, off, 0.02), T.preference(lp, r, None, off, f32(0.02), 0.0, 0.0, False))
+    got = run_policy(bad[0], bad[2], bad[1], bad[3], None, off, kl=0.1, by_seq=True, per_token=True)
+    check_policy(got, T.policy(lp, old, r, adv, None, off, f32(0.2), f32(0.28), f32(0.1), True, True),
+                 loss_size(lp, old, r, adv, None, off, 0.1, True, True))
