@@ -483,6 +483,13 @@ def ckpt_array(ckpts):
     return arr
 
 
+def _per_layer(layers, **arrays):
+    """The library reads as many entries as there are layers."""
+    for name, a in arrays.items():
+        if a is not None and len(a) != len(layers):
+            raise MecefoError(ERR_INVALID_ARG, f"{len(a)} entries in {name}, {len(layers)} layers")
+
+
 def mecefo_stack_ckpt_workspace_bytes(desc, attn, r_gate=0, r_up=0, r_down=0) -> int:
     out = C.c_size_t(0)
     _check(lib().mecefo_stack_ckpt_workspace_bytes(C.byref(desc), C.byref(attn), r_gate, r_up, r_down, C.byref(out)))
@@ -491,12 +498,14 @@ def mecefo_stack_ckpt_workspace_bytes(desc, attn, r_gate=0, r_up=0, r_down=0) ->
 
 def mecefo_stack_fwd_neighbor_ckpt(desc, attn, layers, X0, H, X_out, ws, stream=None):
     """H: ckpt_array(...)."""
+    _per_layer(layers, H=H)
     p, n = _ws(ws)
     _check(lib().mecefo_stack_fwd_neighbor_ckpt(C.byref(desc), C.byref(attn), len(layers), layers, _at(X0), H, _at(X_out),
                                                 p, n, _stream(stream)))
 
 
 def mecefo_stack_bwd_skip_ckpt(desc, layers, H, lowrank, side, dOut_top, dX_bottom, accumulate, ws, stream=None):
+    _per_layer(layers, H=H, lowrank=lowrank)
     p, n = _ws(ws)
     _check(lib().mecefo_stack_bwd_skip_ckpt(C.byref(desc), len(layers), layers, H, lowrank, int(side), _at(dOut_top),
                                             _at(dX_bottom), int(accumulate), p, n, _stream(stream)))

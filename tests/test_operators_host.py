@@ -231,6 +231,10 @@ def test_stack_with_checkpoints_refusals():
     ks = B.ckpt_array([raw_ckpt(), raw_ckpt(ld_q=16)])
     refused(INV, "checkpoint H", B.mecefo_stack_fwd_neighbor_ckpt, d, a, layers, at(), ks, at(512), BIG, STREAM)
     refused(INV, "checkpoint H", B.mecefo_stack_bwd_skip_ckpt, d, layers, ks, (B.LayerLowrank * 2)(), B.SIDE_INPUT, at(), at(512), 0, BIG, STREAM)
+    good = B.ckpt_array([raw_ckpt()])
+    refused(INV, "1 entries in H, 2 layers", B.mecefo_stack_fwd_neighbor_ckpt, d, a, layers, at(), good, at(512), BIG, STREAM)
+    refused(INV, "1 entries in H", B.mecefo_stack_bwd_skip_ckpt, d, layers, good, (B.LayerLowrank * 2)(), B.SIDE_INPUT, at(), at(512), 0, BIG, STREAM)
+    refused(INV, "3 entries in lowrank", B.mecefo_stack_bwd_skip_ckpt, d, layers, ks, (B.LayerLowrank * 3)(), B.SIDE_INPUT, at(), at(512), 0, BIG, STREAM)
     refused(INV, "required", B.mecefo_stack_fwd_neighbor_ckpt, d, a, layers, at(), None, at(512), BIG, STREAM)
     refused(INV, "required", B.mecefo_stack_bwd_skip_ckpt, d, layers, None, (B.LayerLowrank * 2)(), B.SIDE_INPUT, at(), at(512), 0, BIG, STREAM)
     assert B.mecefo_stack_ckpt_workspace_bytes(d, a, 4, 4, 4) >= B.mecefo_block_ckpt_workspace_bytes(d, 4, 4, 4)
