@@ -722,17 +722,20 @@ __global__ __launch_bounds__(Pipe::THREADS, 2) void gemm_bf16_tail_kernel(const 
   const GemmProblem p = product_view<2>(head, kp, 0);
   const int part = e & ((1 << shift) - 1);
   int m0 = tc.tm * BM, n0 = tc.tn * BN_OUT;
-  if (shift == 1) {
+  if (EPI == EPI_HEAD_LSE || shift == 1) {
+    static_assert(EPI != EPI_HEAD_LSE || C2::WN == Cfg::WN, "parts over as many columns as the whole tiles'");
     m0 += part * C2::BM;
     if (m0 < p.M) dtl_tile<C2, P2, AKC, BKC, E, false, false>(head, p, m0, n0, 0, smem);
-  } else if (shift == 2) {
-    m0 += (part >> 1) * C4::BM;
-    n0 += (part & 1) * (BN_OUT / 2);
-    if (m0 < p.M && n0 < p.N) dtl_tile<C4, P4, AKC, BKC, E, false, false>(head, p, m0, n0, 0, smem);
-  } else {
-    m0 += (part >> 2) * C16::BM;
-    n0 += (part & 3) * (BN_OUT / 4);
-    if (m0 < p.M && n0 < p.N) dtl_tile<C16, P16, AKC, BKC, E, false, false>(head, p, m0, n0, 0, smem);
+  } else if constexpr (EPI != EPI_HEAD_LSE) {
+    if (shift == 2) {
+      m0 += (part >> 1) * C4::BM;
+      n0 += (part & 1) * (BN_OUT / 2);
+      if (m0 < p.M && n0 < p.N) dtl_tile<C4, P4, AKC, BKC, E, false, false>(head, p, m0, n0, 0, smem);
+    } else {
+      m0 += (part >> 2) * C16::BM;
+      n0 += (part & 3) * (BN_OUT / 4);
+      if (m0 < p.M && n0 < p.N) dtl_tile<C16, P16, AKC, BKC, E, false, false>(head, p, m0, n0, 0, smem);
+    }
   }
 }
 

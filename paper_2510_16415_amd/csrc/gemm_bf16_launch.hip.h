@@ -14,6 +14,7 @@ using CfgM8 = TileCfg<128, 128, 4, 2>;   // 8 waves x (32 x 64): one workgroup p
 using CfgT = TileCfg<64, 64, 2, 2>;      // 4 waves x (32 x 32): three workgroups per CU
 using CfgX = TileCfg<32, 32, 1, 1>;      // one wave, of eight that share out K
 using CfgH = TileCfg<128, 256, 2, 4>;    // 8 waves x (64 x 64): half a large tile, in the last round of a launch
+using CfgP = TileCfg<128, 256, 4, 2>;    // 8 waves x (32 x 128): the same half where what a wave leaves is over as many columns as a large tile's
 using CfgK = TileCfg<192, 256, 2, 4>;    // 8 waves x (96 x 64): three quarters of one
 
 inline int cdiv(int a, int b) { return (a + b - 1) / b; }
@@ -35,6 +36,7 @@ using PipeL = DtlPipe<CfgL8, 2>;
 using PipeM2 = DtlPipe<CfgM, 2>;
 using PipeM4 = DtlPipe<CfgM8, 4>;   // 128 KiB: one workgroup per CU, three stages in flight
 using PipeH = DtlPipe<CfgH, 3>;    // 144 KiB
+using PipeP = DtlPipe<CfgP, 3>;
 using PipeK = DtlPipe<CfgK, 2>;    // 112 KiB
 using PipeT = DtlPipe<CfgT, 3>;    // 48 KiB
 using PipeT2 = DtlPipe<CfgT, 3, 2>;   // 96 KiB: one workgroup per CU, two groups of waves share out K
@@ -88,7 +90,7 @@ constexpr bool has_tile_k(bool akc, bool bkc, int epi) {
 }
 constexpr bool has_tile_x(int epi) { return epi != EPI_ATTN_P && epi != EPI_ATTN_DS && epi != EPI_ROPE; }
 constexpr bool has_tail(bool akc, bool bkc, int epi) {
-  return (has_tile_k(akc, bkc, epi) && epi != EPI_HEAD_LSE && epi != EPI_HEAD_DU) ||
+  return (has_tile_k(akc, bkc, epi) && epi != EPI_HEAD_DU) ||
          (!akc && !bkc && (epi == EPI_GRAD || epi == EPI_STORE || epi == EPI_HEAD_DW));
 }
 
@@ -126,6 +128,8 @@ inline bool bf16_takes_k(const GemmLaunch& g, bool ragged) {
 // gradients of 360 and 16: 71 / 68, 288 and 24: 92 / 76, 1920 and 4: 147 / 156; bf16 ones: 528 and 8: 61.5 / 52,
 // 1152 and 4: 79 / 85, 336 and 16: 61 / 57.  So below 24 stages only with one or two full rounds, and only where what is saved is more than
 // that.  (forced: wherever it is shorter by the stages alone.)
+// The head's log-sum-exps are cut into halves only, of waves as wide as the whole tile's: [1024 x 4096] x 34000 columns, 532 tiles,
+// 332 / 268; [1024 x 2048] x 50257, 788: 234 / 215; [256 x 4096] x 80000, 313: 248 / 215; [2048 x 2048] x 50257, 1576: 364 / 342.
 struct TailPlan { int tiles, shift, prob; float saved; };
 inline TailPlan bf16_tail(const GemmLaunch& g, bool forced = false) {
   TailPlan plan = {0, 0, 0, 0.f};
@@ -148,7 +152,7 @@ inline TailPlan bf16_tail(const GemmLaunch& g, bool forced = false) {
     if (rounds > 2) return plan;
     lost = g.out_f32 ? 4.f + 0.08f * rest + 1.2f * rounds : 2.f + 0.03f * rest + 0.5f * rounds;
   }
-  for (int k = 0; k < 3; ++k) {
+  for (int k = 0; k < (g.epi == EPI_HEAD_LSE ? 1 : 3); ++k) {      // all its parts are over the same number of columns
     const float saved = 4.f + 1.75f * st - lost - cdiv(rest << shift[k], kCUs) * (4.f + rate[k] * st);
     if (saved > plan.saved) { plan.saved = saved; plan.shift = shift[k]; plan.tiles = rest; }
   }
@@ -328,9 +332,10 @@ hipError_t run_bf16(GemmLaunch& g, hipStream_t stream) {
 template <bool AKC, bool BKC, int EPI>
 struct TailKernel {
   static constexpr int LDS = PipeH::LDS_BYTES;
-  static_assert(LDS >= PipeL::LDS_BYTES && LDS >= PipeM4::LDS_BYTES && LDS >= PipeT2::LDS_BYTES, "the largest of them");
+  static_assert(LDS >= PipeL::LDS_BYTES && LDS >= PipeP::LDS_BYTES && LDS >= PipeM4::LDS_BYTES && LDS >= PipeT2::LDS_BYTES, "the largest of them");
   static auto entry() -> void (*)(const KArgs) {
-    return gemm_bf16_tail_kernel<CfgL8, PipeL, CfgH, PipeH, CfgM8, PipeM4, CfgT, PipeT2, AKC, BKC, EPI>;
+    if constexpr (EPI == EPI_HEAD_LSE) return gemm_bf16_tail_kernel<CfgL8, PipeL, CfgP, PipeP, CfgP, PipeP, CfgP, PipeP, AKC, BKC, EPI>;
+    else return gemm_bf16_tail_kernel<CfgL8, PipeL, CfgH, PipeH, CfgM8, PipeM4, CfgT, PipeT2, AKC, BKC, EPI>;
   }
   static hipError_t prepare() {
     static LdsLimitOnce limit;
@@ -342,6 +347,7 @@ hipError_t run_bf16_tail(GemmLaunch& g, const TailPlan& plan, hipStream_t stream
   using Kern = TailKernel<AKC, BKC, EPI>;
   KArgs a;
   fill_kargs(a, g, CfgL8::BM, epi_is_dual(EPI) ? CfgL8::BN / 2 : CfgL8::BN, kBK);
+  g.part_cols = CfgL8::WN;
   for (int s = 0; s < kMaxProblems; ++s)
     if ((a.h.order >> (4 * s) & 15) == plan.prob) {
       a.h.units[s] -= plan.tiles;

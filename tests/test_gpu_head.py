@@ -197,6 +197,22 @@ def test_every_tile_gives_the_same_to_a_rounding(tile, mecefo_option):
     assert relerr(dX, wX) <= GATE["bf16"] and relerr(dW, wW) <= GATE["bf16"]
 
 
+@pytest.mark.parametrize("tile", ["LT", "auto"])
+@pytest.mark.parametrize("b,d,v,scale", [(1100, 136, 16563, 1.0), (1280, 192, 13500, -0.7), (261, 1024, 35000, 1.0)])
+def test_a_short_last_round_that_is_cut_up(b, d, v, scale, tile, mecefo_option):
+    """More than a round of large tiles, and few in the last one; rows that end in the first half of a tile."""
+    X, W, labels, c = case(b, d, v, "bf16", seed=13, std=d ** -0.5)
+    mecefo_option("tile", tile)
+    mecefo_option("head", "all")
+    logp, L = run_fwd(X, W, labels, "bf16", scale)
+    want, lse = T.head_fwd(X, W, labels, scale)
+    tol = logp_bound(X, W, scale, v)
+    assert (np.abs(logp.cpu().numpy() - want) <= tol).all() and (np.abs(L.cpu().numpy() - lse) <= tol).all()
+    dX, dW, _ = run_bwd(X, W, labels, L, c, "bf16", scale)
+    wX, wW = T.head_bwd(X, W, labels, c, scale)
+    assert relerr(dX, wX) <= GATE["bf16"] and relerr(dW, wW) <= GATE["bf16"]
+
+
 def test_repeats_are_bit_equal_and_streams_do_not_mix():
     X, W, labels, c = case(200, 256, 3000, "bf16", seed=7)
     first = run_fwd(X, W, labels, "bf16")
