@@ -702,22 +702,37 @@ __global__ __launch_bounds__(Pipe::THREADS, 2) void gemm_bf16_tail_kernel(const 
   }
   WorkgroupClock clock;
   clock.start(head);
-  const int bid = blockIdx.x, extra = bid - head.total;
-  if (extra < 0) {
-    int index;
-    const int prob = map_problem(head, bid, &index);
+  const int bid = blockIdx.x;
+  int whole = head.total, cut = head.gemm_blocks - head.total, shift = head.tail >> 24 & 15, first = head.tail & 0xFFFFFF, rows = -1;
+  if constexpr (limits_m(EPI)) {      // rows counted on the device: which round is the last is known here, and a cut one is no more than a round
+    const KProblem kp = load_problem(0);
+    if (kp.C[2]) {
+      rows = limited(kp, kp.M);
+      const int tiles = (uint32_t)(rows + BM - 1) / BM * ((uint32_t)(kp.N + BN_OUT - 1) / BN_OUT), rest = tiles & (kCUs - 1);
+      shift = tiles < kCUs || rest == 0 || rest > kCUs / 2 ? 0 : rest > kCUs / 4 ? 1 : rest > kCUs / 16 ? 2 : 4;
+      whole = first = shift ? tiles - rest : tiles;
+      cut = shift ? rest << shift : 0;
+      if (bid >= whole + cut) return;
+    }
+  }
+  if (bid < whole) {
+    int index = 0, prob = 0;
+    if (rows < 0) prob = map_problem(head, bid, &index);
+    else index = xcd_remap(bid, whole);
     KProblem kp = load_problem(prob);
     if constexpr (limits_k(EPI)) kp.K = limited(kp, kp.K);
+    if (rows >= 0) kp.M = rows;
     const TileCoord tc = map_tile<BM, BN_OUT>(head, kp, prob, index);
     const GemmProblem p = product_view<2>(head, kp, 0);
     dtl_tile<Cfg, Pipe, AKC, BKC, E, false, false>(head, p, tc.tm * BM, tc.tn * BN_OUT, 0, smem);
     clock.stop(head);
     return;
   }
-  const int prob = head.tail >> 28, shift = head.tail >> 24 & 15, first = head.tail & 0xFFFFFF;
-  const int e = xcd_remap(extra, head.gemm_blocks - head.total);
+  const int prob = head.tail >> 28;
+  const int e = xcd_remap(bid - whole, cut);
   KProblem kp = load_problem(prob);
   if constexpr (limits_k(EPI)) kp.K = limited(kp, kp.K);
+  if (rows >= 0) kp.M = rows;
   const TileCoord tc = map_tile<BM, BN_OUT>(head, kp, prob, first + (e >> shift));
   const GemmProblem p = product_view<2>(head, kp, 0);
   const int part = e & ((1 << shift) - 1);

@@ -134,7 +134,7 @@ struct TailPlan { int tiles, shift, prob; float saved; };
 inline TailPlan bf16_tail(const GemmLaunch& g, bool forced = false) {
   TailPlan plan = {0, 0, 0, 0.f};
   if (!has_tail(g.a_kcontig, g.b_kcontig, g.epi) || bf16_ragged(g)) return plan;
-  if (g.epi == EPI_HEAD_GRAD && g.p[0].C[2]) return plan;      // which tiles are the last is not known here
+  if (g.epi == EPI_HEAD_GRAD && g.p[0].C[2]) return plan;      // which tiles are the last is not known here, but to the launch itself
   int total = 0, most = 0;
   for (int i = 0; i < g.nprob; ++i) {
     const GemmProblem& p = g.p[i];
@@ -328,7 +328,9 @@ hipError_t run_bf16(GemmLaunch& g, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// The launch whose last round is cut up as `plan` says.
+// The launch whose last round is cut up as `plan` says, or, without tiles in the plan, as the number of rows says that the
+// workgroups find (kCUs more of them: the parts of the last round are no more than that).  Head backwards with a tenth of the rows
+// out, never cut / cut up, us: [1024 x 2048] x 50257 683 / 671, [4096 x 4096] x 32000 2470 / 2450, [2048 x 2048] x 32000 (no short round) 695 both.
 template <bool AKC, bool BKC, int EPI>
 struct TailKernel {
   static constexpr int LDS = PipeH::LDS_BYTES;
@@ -348,7 +350,7 @@ hipError_t run_bf16_tail(GemmLaunch& g, const TailPlan& plan, hipStream_t stream
   KArgs a;
   fill_kargs(a, g, CfgL8::BM, epi_is_dual(EPI) ? CfgL8::BN / 2 : CfgL8::BN, kBK);
   g.part_cols = CfgL8::WN;
-  for (int s = 0; s < kMaxProblems; ++s)
+  for (int s = 0; s < kMaxProblems && plan.tiles > 0; ++s)
     if ((a.h.order >> (4 * s) & 15) == plan.prob) {
       a.h.units[s] -= plan.tiles;
       a.h.total -= plan.tiles;
@@ -357,7 +359,7 @@ hipError_t run_bf16_tail(GemmLaunch& g, const TailPlan& plan, hipStream_t stream
     }
   const hipError_t e = Kern::prepare();
   if (e != hipSuccess) return e;
-  a.h.gemm_blocks = a.h.total + (plan.tiles << plan.shift);
+  a.h.gemm_blocks = a.h.total + (plan.tiles > 0 ? plan.tiles << plan.shift : kCUs);
   const unsigned side = add_side(a, g, side_kind(AKC, BKC, EPI), PipeL::THREADS);
   hipLaunchKernelGGL(Kern::entry(), dim3(a.h.gemm_blocks + side), dim3(PipeL::THREADS), Kern::LDS, stream, a);
   return hipGetLastError();
@@ -423,7 +425,9 @@ hipError_t run_bf16_auto(GemmLaunch& g, hipStream_t stream) {
       }
       if constexpr (has_tail(AKC, BKC, EPI)) {
         const TailPlan plan = bf16_tail(g, forced == TILE_LT);
-        if (plan.saved > 0.f && (forced < 0 || forced == TILE_LT)) return run_bf16_tail<AKC, BKC, EPI>(g, plan, stream);
+        bool cut = plan.saved > 0.f;
+        if constexpr (limits_m(EPI)) cut |= g.p[0].C[2] && !bf16_ragged(g) && bf16_units(g, 0, 256, 256) > kCUs;
+        if (cut && (forced < 0 || forced == TILE_LT)) return run_bf16_tail<AKC, BKC, EPI>(g, plan, stream);
       }
       if (bf16_ragged(g)) return run_bf16<CfgL8, AKC, BKC, EPI, PipeL, AKC || BKC>(g, stream);
       return run_bf16<CfgL8, AKC, BKC, EPI, PipeL, false>(g, stream);

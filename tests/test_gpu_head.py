@@ -259,6 +259,25 @@ def test_the_list_on_every_tile(tile, b, d, v, mecefo_option):
     assert relerr(dX, wX) <= GATE["bf16"] and relerr(dW, wW) <= GATE["bf16"]
 
 
+@pytest.mark.parametrize("tile", ["auto", "LT"])
+@pytest.mark.parametrize("scored,v", [(1100, 16563), (1024, 16563), (513, 24000), (1100, 13500), (1281, 13570), (20, 16563), (0, 16563), (900, 16384)])
+def test_the_last_round_of_as_many_rows_as_are_listed(scored, v, tile, mecefo_option):
+    """Large tiles of the listed rows: rounds with nothing behind them, with a few tiles, with more than half a round, or not a whole one."""
+    b, d = max(1100, scored), 72
+    X, W, labels, c = case(b, d, v, "bf16", seed=15, skip=0.0, std=d ** -0.5)
+    labels[np.random.default_rng(scored).permutation(b)[scored:]] = -1
+    mecefo_option("head", "scored")
+    mecefo_option("tile", tile)
+    _, L = run_fwd(X, W, labels, "bf16")
+    dX, dW, _ = run_bwd(X, W, labels, L, c, "bf16")
+    wX, wW = T.head_bwd(X, W, labels, c)
+    assert not dX[labels < 0].any()
+    if scored == 0:
+        assert not dW.any()
+    else:
+        assert relerr(dX, wX) <= GATE["bf16"] and relerr(dW, wW) <= GATE["bf16"]
+
+
 def test_the_list_with_a_norm_and_with_few_long_products(mecefo_option):
     mecefo_option("head", "scored")
     for b, d, v in ((300, 64, 20000), (40, 2048, 4000)):      # dU cut along the vocabulary
