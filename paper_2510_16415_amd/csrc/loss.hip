@@ -7,6 +7,8 @@
 // bits, each added up in an order that only the sizes decide.
 #include <math.h>
 
+#include <type_traits>
+
 #include "../../include/mecefo.h"
 #include "loss_ranges.h"
 #include "mecefo_internal.h"
@@ -20,7 +22,8 @@ constexpr int kThreads = 256;
 // 18.8, 24.0; 8 of 1000 6.9, 8.7 / 8.3, 9.8 / 8.4, 9.8.
 constexpr int kSliceTokens = 512;
 constexpr int kMaxSlices = 256;
-constexpr int kWaveSlices = 16;      // from here on a wave adds up a sequence's slices, below a thread does
+constexpr int kRowSlices = 16;       // from here on 16 lanes add up a sequence's slices, below a thread does
+constexpr int kRowSeqs = 128;        // batches of so many slices have about 4 * kCUs / (kRowSlices - 1) sequences at most
 // One workgroup and one launch: a wave to a sequence.  GPU time of one launch / two, us: preference 8 x 64 tokens 6.0 / 6.6, 8 x 250
 // 7.5 / 6.6, 64 x 16 13.1 / 6.7, 512 x 8 72 / 7.7; policy 2 x 100 8.1 / 7.5.  Calls that a program makes one by one, the launches among
 // them: preference 2 x 20 to 16 x 32 7.6 to 8.1 / 11.4, policy 8.0 to 10 / 11.5.
@@ -85,11 +88,19 @@ struct PrefArgs {
   double beta, smooth, margin, grad_scale;
 };
 
-// The slices of one sequence added up by a wave, in all its lanes, or by a thread.
+// The slices of one sequence added up by a wave or by 16 lanes, in all of them, or by a thread.
 __device__ inline Part wave_slices(const Part* p, int n) {
   Part s = {0.0, 0.0};
   for (int j = threadIdx.x & 63; j < n; j += 64) { s.sum += p[j].sum; s.count += p[j].count; }
   return Part{wave_sum(s.sum), wave_sum(s.count)};
+}
+__device__ inline Part row_slices(const Part* p, int n) {
+  Part s = {0.0, 0.0};
+#pragma unroll 4
+  for (int j = threadIdx.x & 15; j < n; j += 16) { const Part x = p[j]; s.sum += x.sum; s.count += x.count; }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) { s.sum += __shfl_xor(s.sum, o, 64); s.count += __shfl_xor(s.count, o, 64); }
+  return s;
 }
 __device__ inline Part thread_slices(const Part* p, int n) {
   Part s = {0.0, 0.0};
@@ -152,8 +163,9 @@ __device__ inline void clear_outside(const int64_t* offsets, int64_t tokens, int
 }
 
 // Workgroups 0 .. 2 * pairs * slices - 1: the gradients of a slice; the one behind them: the mean loss, every pair's margin and
-// rewards; the last ones: the tokens of no sequence.  The one takes a wave to a pair where sequences have many slices, else a thread (64 pairs
-// of 4 slices: the launch 28 us with a wave to a pair, 6 with a thread).
+// rewards; the last ones: the tokens of no sequence.  The one takes a thread to a pair (64 pairs of 4
+// slices: the launch 28 us with a wave to a pair, 6 with a thread), and 16 lanes to a sequence first where it has many slices (32 pairs of 16
+// slices: the call 28.6 us with a wave to a pair, 18.5).
 __global__ __launch_bounds__(kThreads) void preference_grad_kernel(const PrefArgs a) {
   const int grads = 2 * a.pairs * a.slices;
   if ((int)blockIdx.x == grads) {
@@ -167,11 +179,14 @@ __global__ __launch_bounds__(kThreads) void preference_grad_kernel(const PrefArg
     };
     const Part* parts = a.parts;
     const int n = a.slices;
-    if (n >= kWaveSlices) {
-      for (int i = threadIdx.x >> 6; i < a.pairs; i += kThreads / 64) {
-        const Part c = wave_slices(parts + (int64_t)(2 * i) * n, n), o = wave_slices(parts + (int64_t)(2 * i + 1) * n, n);
-        if ((threadIdx.x & 63) == 0) pair(i, c, o);
+    if (n >= kRowSlices && 2 * a.pairs <= kRowSeqs) {
+      __shared__ Part sums[kRowSeqs];
+      for (int k = threadIdx.x >> 4; k < 2 * a.pairs; k += kThreads / 16) {
+        const Part p = row_slices(parts + (int64_t)k * n, n);
+        if ((threadIdx.x & 15) == 0) sums[k] = p;
       }
+      __syncthreads();
+      if ((int)threadIdx.x < a.pairs) pair(threadIdx.x, sums[2 * threadIdx.x], sums[2 * threadIdx.x + 1]);
     } else {
       for (int i = threadIdx.x; i < a.pairs; i += kThreads)
         pair(i, thread_slices(parts + (int64_t)(2 * i) * n, n), thread_slices(parts + (int64_t)(2 * i + 1) * n, n));
@@ -320,16 +335,24 @@ __global__ __launch_bounds__(kThreads) void policy_tokens_kernel(const PolicyArg
   a.counts[blockIdx.x] = (uint32_t)t[3];
 }
 
-// Workgroup seqs * slices: the results; those behind it: the tokens of no sequence.
+// Workgroup seqs * slices: the results; those behind it: the tokens of no sequence.  Sequences of many slices are added up by 16
+// lanes each, where there are no more than four by a wave each (means over sequences, us, a wave each / this: 64 sequences of 16000 tokens 41.5 / 22.5, 16 of
+// 60000 23.4 / 18.4, 2 of 200000 15.2 / 13.5).
 __global__ __launch_bounds__(kThreads) void policy_scale_kernel(const PolicyArgs a) {
-  const int grads = a.seqs * a.slices, k = blockIdx.x / a.slices, j = blockIdx.x - k * a.slices, lane = threadIdx.x & 63;
+  const int grads = a.seqs * a.slices, k = blockIdx.x / a.slices, j = blockIdx.x - k * a.slices;
   if ((int)blockIdx.x > grads) return clear_outside(a.offsets, a.tokens, a.seqs, a.dlogp, blockIdx.x - grads - 1, gridDim.x - grads - 1);
-  const bool total = (int)blockIdx.x == grads, waves = a.slices >= kWaveSlices;
-  auto wave_count = [&](int i) {
-    double c = 0.0;
-    for (int q = lane; q < a.slices; q += 64) c += a.counts[i * a.slices + q];
-    return wave_sum(c);
+  const bool total = (int)blockIdx.x == grads, rows = a.slices >= kRowSlices;
+  auto lanes_count = [&](int i, auto of) {
+    constexpr int lanes = decltype(of)::value;
+    uint32_t c = 0;
+#pragma unroll 4
+    for (int q = threadIdx.x & (lanes - 1); q < a.slices; q += lanes) c += a.counts[i * a.slices + q];
+#pragma unroll
+    for (int o = lanes / 2; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
+    return (double)c;
   };
+  using Wave = std::integral_constant<int, 64>;
+  using Row = std::integral_constant<int, 16>;      // lanes to a sequence of many slices, where there are more than four
   auto thread_count = [&](int i) {
     uint32_t c = 0;
 #pragma unroll 4
@@ -341,8 +364,13 @@ __global__ __launch_bounds__(kThreads) void policy_scale_kernel(const PolicyArgs
     double n = 0.0;
     if (!a.by_sequence) {
       for (int i = threadIdx.x; i < grads; i += kThreads) n += a.counts[i];
-    } else if (waves) {
-      for (int i = threadIdx.x >> 6; i < a.seqs; i += kThreads / 64) n += wave_count(i) > 0.0 && lane == 0 ? 1.0 : 0.0;
+    } else if (rows) {
+      auto live = [&](auto of) {
+        constexpr int L = decltype(of)::value;
+        for (int i = threadIdx.x / L; i < a.seqs; i += kThreads / L) n += lanes_count(i, of) > 0.0 && threadIdx.x % L == 0 ? 1.0 : 0.0;
+      };
+      if (a.seqs <= 4) live(Wave{});
+      else live(Row{});
     } else {
       for (int i = threadIdx.x; i < a.seqs; i += kThreads) n += thread_count(i) > 0.0 ? 1.0 : 0.0;
     }
@@ -350,7 +378,7 @@ __global__ __launch_bounds__(kThreads) void policy_scale_kernel(const PolicyArgs
   };
   if (!total) {
     const TokenRange r = token_slice(sequence(a.offsets, a.tokens, k), j, a.slices);
-    return scale_gradients(a, r, threadIdx.x, kThreads, [&]() { return (float)token_weight(a, all(), a.by_sequence ? wave_count(k) : 0.0); });
+    return scale_gradients(a, r, threadIdx.x, kThreads, [&]() { return (float)token_weight(a, all(), a.by_sequence ? lanes_count(k, Wave{}) : 0.0); });
   }
   const double n = all();
   double t[3] = {0.0, 0.0, 0.0};
@@ -361,11 +389,17 @@ __global__ __launch_bounds__(kThreads) void policy_scale_kernel(const PolicyArgs
     const double w = token_weight(a, n, 0.0);
 #pragma unroll 2
     for (int q = threadIdx.x; q < grads; q += kThreads) add(q, w);
-  } else if (waves) {
-    for (int i = threadIdx.x >> 6; i < a.seqs; i += kThreads / 64) {
-      const double w = token_weight(a, n, wave_count(i));
-      for (int q = lane; q < a.slices; q += 64) add(i * a.slices + q, w);
-    }
+  } else if (rows) {
+    auto weighted = [&](auto of) {
+      constexpr int L = decltype(of)::value;
+      for (int i = threadIdx.x / L; i < a.seqs; i += kThreads / L) {
+        const double w = token_weight(a, n, lanes_count(i, of));
+#pragma unroll 2
+        for (int q = threadIdx.x % L; q < a.slices; q += L) add(i * a.slices + q, w);
+      }
+    };
+    if (a.seqs <= 4) weighted(Wave{});
+    else weighted(Row{});
   } else {
     for (int i = threadIdx.x; i < a.seqs; i += kThreads) {
       const double w = token_weight(a, n, thread_count(i));

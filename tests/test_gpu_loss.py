@@ -210,3 +210,18 @@ def test_tokens_of_no_sequence_get_zeros(front, used, behind):
     got = run_policy(bad[0], bad[2], bad[1], bad[3], None, off, kl=0.1, by_seq=True, per_token=True)
     check_policy(got, T.policy(lp, old, r, adv, None, off, f32(0.2), f32(0.28), f32(0.1), True, True),
                  loss_size(lp, old, r, adv, None, off, 0.1, True, True))
+
+
+@pytest.mark.parametrize("seqs,mean_len", [(24, 8200), (4, 33000), (34, 9000)])
+def test_few_sequences_of_many_slices(seqs, mean_len):
+    rng = np.random.default_rng([seqs, mean_len])
+    off = offsets(rng, seqs, mean_len, front=1)
+    lp, old, r, mask = arrays(rng, int(off[-1]) + 2, 0.3)
+    beta = 0.3 / np.sqrt(mean_len)
+    got = run_preference(spoil(lp, mask, rng), spoil(r, mask, rng), mask, off, beta)
+    check_preference(got, T.preference(lp, r, mask, off, f32(beta), 0.0, 0.0, False))
+    adv = rng.standard_normal(seqs).astype(np.float32)
+    for by_seq in (False, True):
+        got = run_policy(spoil(lp, mask, rng), spoil(old, mask, rng), spoil(r, mask, rng), adv, mask, off, kl=0.05, by_seq=by_seq)
+        check_policy(got, T.policy(lp, old, r, adv, mask, off, f32(0.2), f32(0.28), f32(0.05), by_seq),
+                     loss_size(lp, old, r, adv, mask, off, 0.05, by_seq, False))
