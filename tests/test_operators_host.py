@@ -254,12 +254,14 @@ def test_ranges_of_sequences_and_slices(tmp_path):
 def test_head_option():
     refused(INV, "option head", B.mecefo_set_option, "head", "some")
     h = head(tokens=4096, d_model=1024, vocab=32000)
-    need = {}
+    narrow = head(tokens=131072, d_model=512, vocab=1000)      # as many operations, a vocabulary too small for a list to pay
+    need, small = {}, {}
     try:
         for v in ("all", "scored", "auto"):
             B.mecefo_set_option("head", v)
+            small[v] = B.mecefo_head_workspace_bytes(narrow, True)
             need[v] = B.mecefo_head_workspace_bytes(h, True), B.mecefo_head_workspace_bytes(head(), True), B.mecefo_head_workspace_bytes(h, False)
     finally:
         B.mecefo_set_option("head", "auto")
     assert need["auto"][0] == need["scored"][0] >= need["all"][0] + 4096 * (1024 * 2 + 20) and need["auto"][1] == need["all"][1] < need["scored"][1]
-    assert len({n[2] for n in need.values()}) == 1
+    assert len({n[2] for n in need.values()}) == 1 and small["auto"] == small["all"] < small["scored"]
