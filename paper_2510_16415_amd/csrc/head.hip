@@ -85,11 +85,11 @@ __global__ __launch_bounds__(1024) void head_parts_kernel(const float2* __restri
 }
 
 // out[row, 0 .. cols) = sum of the parts [k][row, col], in their order, V columns per thread.  list: the rows are *count in
-// number, and row r goes to row list[r].
+// number, and row r goes to row list[r].  accumulate: added to what is there.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void head_sum_kernel(const float* __restrict__ part, int parts, int64_t rows, int cols,
                                                        T* __restrict__ out, int64_t ldo, const int* __restrict__ list,
-                                                       const int* __restrict__ count) {
+                                                       const int* __restrict__ count, int accumulate) {
   if (list) rows = *count;
   struct alignas(4 * V) In { float e[V]; };
   struct alignas(sizeof(T) * V) Out { T e[V]; };
@@ -103,10 +103,16 @@ __global__ __launch_bounds__(256) void head_sum_kernel(const float* __restrict__
 #pragma unroll
     for (int e = 0; e < V; ++e) s.e[e] += x.e[e];
   }
+  Out* to = (Out*)(out + (list ? (int64_t)list[row] : row) * ldo + (i - row * cols));
   Out o;
+  if (accumulate) {
+    o = *to;
+#pragma unroll
+    for (int e = 0; e < V; ++e) s.e[e] += (float)o.e[e];
+  }
 #pragma unroll
   for (int e = 0; e < V; ++e) o.e[e] = (T)s.e[e];
-  *(Out*)(out + (list ? (int64_t)list[row] : row) * ldo + (i - row * cols)) = o;
+  *to = o;
 }
 
 // The rows that take part in the gradient, a label in the vocabulary and a dlogp that is not zero, in their order at the front
@@ -328,6 +334,19 @@ mecefo_status_t head_norm(const Head& h, const HeadWs& w, char* base, const void
   return MECEFO_OK;
 }
 
+hipError_t sum_parts(bool bf16, const void* part, int parts, int64_t rows, int cols, void* out, int64_t ldo, const int* list, const int* count,
+                     int accumulate, hipStream_t s) {
+  auto go = [&](auto type, auto v) {
+    using T = decltype(type);
+    constexpr int V = decltype(v)::value;
+    hipLaunchKernelGGL((head_sum_kernel<T, V>), dim3((unsigned)((rows * cols / V + 255) / 256)), dim3(256), 0, s, (const float*)part, parts, rows, cols, (T*)out, ldo, list, count, accumulate);
+  };
+  if (bf16) go(__bf16{}, std::integral_constant<int, 4>{});      // rows are whole vectors of eight
+  else if (cols % 4 == 0 && ldo % 4 == 0 && (uintptr_t)out % 16 == 0) go(float{}, std::integral_constant<int, 4>{});
+  else go(float{}, std::integral_constant<int, 1>{});
+  return hipGetLastError();
+}
+
 }  // namespace
 }  // namespace mecefo
 
@@ -428,12 +447,24 @@ mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const vo
     p.scale = desc->logit_scale;
     HIP_TRY(launch_gemm(g, s));
   }
-  {  // dW = dz^T U   [V x d], contraction over tokens
-    GemmLaunch g = product(h, false, false, list ? EPI_HEAD_DW : EPI_GRAD, dZ, h.ldz, U, ldu, dW, desc->ld_w, h.vocab, h.dm, h.b);
-    g.p[0].C[2] = count;
-    g.out_f32 = grad_f32;
-    g.accumulate = accumulate;
+  {  // dW = dz^T U   [V x d], contraction over tokens, cut where there are many to a small dW (by the list their number is not known here)
+    GemmLaunch g = product(h, false, false, EPI_STORE, dZ, h.ldz, U, ldu, base + w.part, h.dm, h.vocab, h.dm, h.b);
+    if (any && !list) {
+      const int64_t most = w.room / ((int64_t)h.vocab * h.dm);
+      if (h.bf16) bf16_plan_splits(g, w.room);
+      else f32_plan_splits(g, (int)(most < kMaxParts ? most : kMaxParts));
+    }
+    const int parts = g.p[0].splits;
+    if (parts < 2) {
+      g.epi = list ? EPI_HEAD_DW : EPI_GRAD;
+      g.p[0].C[0] = dW;
+      g.p[0].C[2] = count;
+      g.p[0].ldc = desc->ld_w;
+      g.out_f32 = grad_f32;
+      g.accumulate = accumulate;
+    }
     HIP_TRY(launch_gemm(g, s));
+    if (parts > 1) HIP_TRY(sum_parts(!grad_f32, base + w.part, parts, h.vocab, h.dm, dW, desc->ld_w, nullptr, nullptr, accumulate, s));
   }
   int nblk = 0;
   float* dgp = (float*)(base + w.dgp);
@@ -448,19 +479,7 @@ mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const vo
     if (parts > 1) g.p[0].C[0] = base + w.part;
     else g.p[0].ldc = lddu;
     HIP_TRY(launch_gemm(g, s));
-    if (parts > 1) {
-      const float* part = (const float*)(base + w.part);
-      const int64_t n = (int64_t)h.b * h.dm;
-      auto sum = [&](auto type, auto v) {      // bf16 rows are whole vectors of eight
-        using T = decltype(type);
-        constexpr int V = decltype(v)::value;
-        hipLaunchKernelGGL((head_sum_kernel<T, V>), dim3((unsigned)((n / V + 255) / 256)), dim3(256), 0, s, part, parts, (int64_t)h.b, h.dm, (T*)dU, lddu, list, count);
-      };
-      if (h.bf16) sum(__bf16{}, std::integral_constant<int, 4>{});
-      else if (h.dm % 4 == 0 && lddu % 4 == 0 && (uintptr_t)dU % 16 == 0) sum(float{}, std::integral_constant<int, 4>{});
-      else sum(float{}, std::integral_constant<int, 1>{});
-      HIP_TRY(hipGetLastError());
-    }
+    if (parts > 1) HIP_TRY(sum_parts(h.bf16, base + w.part, parts, h.b, h.dm, dU, lddu, list, count, 0, s));
     if (gamma) {  // dX = normbwd(dU): the norm backward adds a residual gradient, here a row of zeros with stride 0
       const int words = (h.dm * h.esz + 3) / 4;
       hipLaunchKernelGGL(head_zero_kernel, dim3((words + 255) / 256), dim3(256), 0, s, (uint32_t*)(base + w.zero), words);

@@ -213,6 +213,26 @@ def test_a_short_last_round_that_is_cut_up(b, d, v, scale, tile, mecefo_option):
     assert relerr(dX, wX) <= GATE["bf16"] and relerr(dW, wW) <= GATE["bf16"]
 
 
+@pytest.mark.parametrize("dtype,grad,gamma", [("bf16", "f32", False), ("bf16", "bf16", True), ("f32", "f32", False), ("f32", "f32", True)])
+@pytest.mark.parametrize("b,d,v", [(6000, 64, 40), (5000, 72, 257), (9001, 16, 3)])
+def test_many_tokens_and_a_small_vocabulary(b, d, v, dtype, grad, gamma):
+    """dW cut along the tokens; strides, and a gradient that is added to."""
+    X, W, labels, c = case(b, d, v, dtype, seed=21)
+    g = np.ones(d, np.float32) if gamma else None
+    x = X.astype(np.float64)
+    U = x / np.sqrt((x * x).mean(axis=1, keepdims=True) + float(np.float32(1e-6))) if gamma else x
+    if gamma and dtype == "bf16":
+        U = I.round_to_bf16_grid(U).astype(np.float64)
+    _, L = run_fwd(X, W, labels, dtype, gamma=g, pad=8)
+    _, dW, _ = run_bwd(X, W, labels, L, c, dtype, gamma=g, pad=8, grad=grad)
+    wW = T.head_bwd(U, W, labels, c)[1]
+    gate = 4 * 2.0 ** -8 if gamma and dtype == "bf16" else GATE[dtype]      # as with a norm elsewhere
+    assert relerr(dW, wW) <= gate
+    more = run_bwd(X, W, labels, L, c, dtype, gamma=g, pad=8, grad=grad, accumulate=1)[1]
+    step = 2.0 ** -8 if grad == "bf16" else U32
+    assert (np.abs(more - (dW + 0.25)) <= step * (np.abs(dW) + np.abs(more) + 0.25)).all()
+
+
 def test_repeats_are_bit_equal_and_streams_do_not_mix():
     X, W, labels, c = case(200, 256, 3000, "bf16", seed=7)
     first = run_fwd(X, W, labels, "bf16")
