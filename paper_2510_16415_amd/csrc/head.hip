@@ -249,13 +249,14 @@ constexpr int64_t kPartRoom = 32 << 20;      // fp32 elements
 // rows these are is known on the device alone; two launches and the copy cost 10 to 20 us, which is 0.4 % of the largest calls.  All rows /
 // the list, us, with none, a tenth and three tenths of the tokens out: [8192 x 4096], vocabulary 32000, 5240 / 5259, 5211 / 4966,
 // 5151 / 4237; [2048 x 2048] 735 / 735, 730 / 701, 720 / 579; [1024 x 1024] (2e11 operations) 232 / 231, 219 / 222, 219 / 194; [512 x 2048]
-// 227 / 236, 225 / 228, 223 / 213; [1024 x 512] (1e11) 140 / 150, 140 / 146, 140 / 133.  The list and the copy cost a row about 1 ns + d / 1000 ns,
-// its products 6 d V operations, so the vocabulary decides too: a tenth out, 16384 x 1024, V 4096 456 / 443; 32768 x 1024, V 2048 501 / 560;
-// 131072 x 512, V 1000 1072 / 1188.  In fp32 all rows.
+// 227 / 236, 225 / 228, 223 / 213; [1024 x 512] (1e11) 140 / 150, 140 / 146, 140 / 133.  And only where
+// dW has about a 256 x 256 tile for every CU: with fewer it is cut along the tokens, which a number of rows that the host does not know rules out.
+// A tenth out, us: 16384 x 1024, V 4096 401 / 449; 65536 x 512, V 8192 1733 / 1991; 8192 x 1024, V 8192 392 / 411; 16384 x 2048, V 8192
+// 1336 / 1289; 65536 x 1024, V 16000 5781 / 5701; 32768 x 512, V 32000 3582 / 3291.  In fp32 all rows.
 bool by_list(const Head& h) {
   if (!h.bf16) return false;
   const int forced = options().head_rows.load(std::memory_order_relaxed);
-  return forced ? forced == 2 : h.vocab >= 4096 && 6.0 * h.b * h.dm * h.vocab >= 2e11;
+  return forced ? forced == 2 : (int64_t)h.vocab * h.dm >= 16000000 && 6.0 * h.b * h.dm * h.vocab >= 2e11;
 }
 
 struct HeadWs {

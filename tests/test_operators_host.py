@@ -254,7 +254,7 @@ def test_ranges_of_sequences_and_slices(tmp_path):
 def test_head_option():
     refused(INV, "option head", B.mecefo_set_option, "head", "some")
     h = head(tokens=4096, d_model=1024, vocab=32000)
-    narrow = head(tokens=131072, d_model=512, vocab=1000)      # as many operations, a vocabulary too small for a list to pay
+    narrow = head(tokens=131072, d_model=512, vocab=1000)      # as many operations, dW too small for a list to pay
     need, small = {}, {}
     try:
         for v in ("all", "scored", "auto"):
