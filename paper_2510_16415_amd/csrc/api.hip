@@ -167,7 +167,7 @@ struct StageTimer {
 // ---- workspace ------------------------------------------------------------------------
 struct Workspace {
   // offsets in bytes from the (256-byte aligned) workspace base
-  size_t U, rstd, DG, DZ, AA, dU, T[3], C[3], partial, dgp, parts, total;
+  size_t U, rstd, DG, DZ, AA, dU, T[3], C[3], partial, dgp, parts, end, total;
   int64_t room, parts_room;      // fp32 elements of the partial buffer, and of the one that keeps the parts of dU
   int splits;
   int64_t c_elems[3];
@@ -279,13 +279,14 @@ Workspace layout(const Ctx& c, const int r[3], mecefo_side_t side, int force_spl
   w.dgp = take((size_t)rmsnorm_bwd_blocks(c.b) * c.dm * 4);
   w.parts_room = with_parts ? kept_parts(c) * c.b * c.dm : 0;
   w.parts = take((size_t)w.parts_room * 4);
+  w.end = off;
   w.total = off + 256;   // slack for aligning the caller's base pointer
   return w;
 }
 
 struct Bufs { char* base; Workspace w; };
 
-// tail: bytes that the caller needs behind the layout.
+// tail: bytes that the caller needs behind the layout, from its end on.
 mecefo_status_t carve(const Ctx& c, const int r[3], mecefo_side_t side, void* ws, size_t ws_bytes, Bufs* out, size_t tail = 0) {
   Workspace w = layout(c, r, side, 0, true);
   if (w.total + tail > ws_bytes) w = layout(c, r, side, 0, false);
@@ -770,7 +771,7 @@ mecefo_status_t block_bwd_skip(const mecefo_ffn_desc_t* desc, const void* H, con
   int64_t ldh = desc->ld_act_d;
   const bool unpack = kept && c.b > 0;
   if (unpack) {
-    void* Hk = base + bf.w.total;      // the layout's slack of 256 bytes lies in front
+    void* Hk = base + bf.w.end;      // the slack that the layout's total has belongs in front of the base
     STAGE(MECEFO_STAGE_NORM_FWD, s);
     if (gamma) HIP_TRY(launch_rmsnorm_ckpt(c.bf16, kh, gamma, desc->rms_eps, Hk, base + bf.w.U, (float*)(base + bf.w.rstd), c.b, c.dm, s));
     else HIP_TRY(launch_ckpt_unpack(c.bf16, kh, c.b, c.dm, Hk, c.dm, s));
