@@ -267,32 +267,68 @@ __device__ inline float exp_excess(float q) {
   return s * q * q;
 }
 
-// The tokens of a range: their gradients without the weight, and a thread's share of the sums.
 struct PolicyToken { float logp, old, ref, A; uint8_t on; };
+__device__ inline PolicyToken policy_token(const PolicyArgs& a, int64_t t, int k) {
+  return PolicyToken{a.logp[t], a.old[t], a.ref ? a.ref[t] : 0.f, a.advantage[a.per_token ? t : k], a.mask ? a.mask[t] : (uint8_t)1};
+}
+// Which side of a bound the ratio lies on is decided by the difference itself, in 64 bits.
+__device__ inline bool policy_over(const PolicyArgs& a, float A, double diff) {
+  return (A > 0.f && diff > a.log_high) || (A < 0.f && diff < a.log_low);
+}
+
+// A counted token's terms where fp32 does not hold one of them: exp(88.8) is beyond it.  An exponential that fp32 holds is taken as
+// the other tokens have it; the others stay below infinity, so that a ratio without an advantage and a KL term without a
+// coefficient are zero at any distance.
+struct PolicyTerms { double loss, kl, grad; };
+__device__ inline PolicyTerms policy_far(const PolicyArgs& a, const PolicyToken& x) {
+  auto power = [](double v) {      // a NaN stays one
+    const float near = expf((float)v);
+    const double far = near < INFINITY ? (double)near : exp(v);
+    return far > 1.7976931348623157e308 ? 1.7976931348623157e308 : far;
+  };
+  const double diff = (double)x.logp - (double)x.old, A = x.A, q = a.ref ? (double)x.ref - (double)x.logp : 0.0;
+  const bool over = policy_over(a, x.A, diff);
+  const double rho = power(diff), kept = over ? (x.A > 0.f ? a.high : a.low) : rho;
+  const float near = exp_excess((float)q);
+  const double excess = near < INFINITY ? (double)near : power(q) - 1.0 - q;      // |q| is large
+  return PolicyTerms{a.kl_coef * excess - kept * A, excess, a.grad_scale * ((over ? 0.0 : -rho * A) - a.kl_coef * (q + excess))};
+}
+
+// The tokens of a range: their gradients without the weight, and a thread's share of the sums.
 __device__ inline PolicySums policy_tokens(const PolicyArgs& a, TokenRange r, int first, int stride, int k) {
   PolicySums s = {0.0, 0.0, 0.0, 0};
-  for_tokens(r, first, stride,
-             [&](int64_t t) {
-               return PolicyToken{a.logp[t], a.old[t], a.ref ? a.ref[t] : 0.f, a.advantage[a.per_token ? t : k],
-                                  a.mask ? a.mask[t] : (uint8_t)1};
-             },
+  bool far = false;      // of some tokens fp32 does not hold a term: they get a NaN, and their turn behind the loop
+  for_tokens(r, first, stride, [&](int64_t t) { return policy_token(a, t, k); },
              [&](int64_t t, const PolicyToken& x) {
                float g = 0.f;
                if (x.on) {
-                 // which side of a bound the ratio lies on is decided by the difference itself, in 64 bits
                  const double diff = (double)x.logp - (double)x.old;
-                 const bool over = (x.A > 0.f && diff > a.log_high) || (x.A < 0.f && diff < a.log_low);
+                 const bool over = policy_over(a, x.A, diff);
                  const float rho = expf((float)diff);
                  const double kept = over ? (x.A > 0.f ? a.high : a.low) : (double)rho;
                  const float q = a.ref ? (float)((double)x.ref - (double)x.logp) : 0.f, excess = exp_excess(q);
                  g = a.grad_scale * ((over ? 0.f : -rho * x.A) - a.kl_coef * (q + excess));      // exp(q) - 1
-                 s.loss += (double)a.kl_coef * excess - kept * x.A;      // the clipped terms are all of one size: a rounding of it would add up
-                 s.kl += (double)excess;
+                 if (rho + excess + fabsf(g) < INFINITY) {
+                   s.loss += (double)a.kl_coef * excess - kept * x.A;      // the clipped terms are all of one size: a rounding of it would add up
+                   s.kl += (double)excess;
+                 } else {
+                   g = __builtin_nanf("");
+                   far = true;
+                 }
                  s.clipped += over ? 1.0 : 0.0;
                  s.count += 1;
                }
                a.dlogp[t] = g;
              });
+  if (far)
+#pragma unroll 1
+    for (int64_t t = r.lo + first; t < r.hi; t += stride)
+      if (isnan(a.dlogp[t])) {
+        const PolicyTerms f = policy_far(a, policy_token(a, t, k));
+        a.dlogp[t] = (float)f.grad;
+        s.loss += f.loss;
+        s.kl += f.kl;
+      }
   return s;
 }
 // What the tokens' weights are made of: over all sequences their counted tokens, or how many have any (by_sequence).
