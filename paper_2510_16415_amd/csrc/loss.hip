@@ -338,17 +338,31 @@ __device__ inline double token_weight(const PolicyArgs& a, double n, double own)
   const double c = a.by_sequence ? n * own : n;
   return c > 0.0 ? 1.0 / c : 0.0;
 }
+// A gradient without the weight that is beyond fp32 may be back in it with the weight: it is formed again in 64 bits.
 template <class W>
-__device__ inline void scale_gradients(const PolicyArgs& a, TokenRange r, int first, int stride, W weight) {
+__device__ inline void scale_gradients(const PolicyArgs& a, TokenRange r, int first, int stride, int k, W weight) {
   const int64_t t0 = r.lo + first;
   float g[kAhead];
 #pragma unroll
   for (int u = 0; u < kAhead; ++u) g[u] = t0 + (int64_t)u * stride < r.hi ? a.dlogp[t0 + (int64_t)u * stride] : 0.f;
-  const float w = weight();
+  const double weight64 = weight();
+  const float w = (float)weight64;
+  bool far = false;
 #pragma unroll
   for (int u = 0; u < kAhead; ++u)
-    if (t0 + (int64_t)u * stride < r.hi) a.dlogp[t0 + (int64_t)u * stride] = g[u] * w;
-  for_tokens(r, first + kAhead * stride, stride, [&](int64_t t) { return a.dlogp[t]; }, [&](int64_t t, float x) { a.dlogp[t] = x * w; });
+    if (t0 + (int64_t)u * stride < r.hi) {
+      far |= isinf(g[u]);
+      a.dlogp[t0 + (int64_t)u * stride] = g[u] * w;
+    }
+  for_tokens(r, first + kAhead * stride, stride, [&](int64_t t) { return a.dlogp[t]; },
+             [&](int64_t t, float x) {
+               far |= isinf(x);
+               a.dlogp[t] = x * w;
+             });
+  if (far)
+#pragma unroll 1
+    for (int64_t t = t0; t < r.hi; t += stride)
+      if (isinf(a.dlogp[t])) a.dlogp[t] = (float)(policy_far(a, policy_token(a, t, k)).grad * weight64);
 }
 __device__ inline void policy_results(const PolicyArgs& a, double loss, double kl, double clipped) {
   a.loss[0] = (float)loss;
@@ -414,7 +428,7 @@ __global__ __launch_bounds__(kThreads) void policy_scale_kernel(const PolicyArgs
   };
   if (!total) {
     const TokenRange r = token_slice(sequence(a.offsets, a.tokens, k), j, a.slices);
-    return scale_gradients(a, r, threadIdx.x, kThreads, [&]() { return (float)token_weight(a, all(), a.by_sequence ? lanes_count(k, Wave{}) : 0.0); });
+    return scale_gradients(a, r, threadIdx.x, kThreads, k, [&]() { return token_weight(a, all(), a.by_sequence ? lanes_count(k, Wave{}) : 0.0); });
   }
   const double n = all();
   double t[3] = {0.0, 0.0, 0.0};
@@ -464,7 +478,7 @@ __global__ __launch_bounds__(1024) void policy_small_kernel(const PolicyArgs a) 
   double t[3] = {0.0, 0.0, 0.0};
   for (int k = wave; k < a.seqs; k += 16) {
     const double w = token_weight(a, n, sums[k].count);
-    scale_gradients(a, sequence(a.offsets, a.tokens, k), lane, 64, [&]() { return (float)w; });
+    scale_gradients(a, sequence(a.offsets, a.tokens, k), lane, 64, k, [&]() { return w; });
     if (lane == 0) { t[0] += sums[k].loss * w; t[1] += sums[k].kl * w; t[2] += sums[k].clipped * w; }
   }
   clear_outside(a.offsets, a.tokens, a.seqs, a.dlogp, 0, 1);

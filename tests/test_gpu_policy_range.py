@@ -85,3 +85,35 @@ def test_what_is_not_a_number_stays_one():
     lp = np.array([np.nan, -1, -2], np.float32)
     got = run_policy(lp, np.full(3, -1, np.float32), None, np.zeros(1, np.float32), None, np.array([0, 3], np.int64))
     assert np.isnan(got["loss"][0]) and np.isnan(got["dlogp"]).tolist() == [True, False, False]
+
+
+@pytest.mark.parametrize("by_seq", [False, True])
+@pytest.mark.parametrize("seqs,mean_len", [(16, 30), (1, 700), (40, 600), (3, 30000)])
+def test_a_gradient_that_its_weight_brings_back_into_fp32(seqs, mean_len, by_seq):
+    """rho A, the KL term and grad_scale times either beyond 3.4e38, their share of the batch below it."""
+    rng = np.random.default_rng([seqs, mean_len, int(by_seq), 3])
+    off = (1 + np.arange(seqs + 1) * mean_len).astype(np.int64)
+    n, every = int(off[-1]) + 2, seqs * mean_len
+    top = np.log(3.4e38) + 0.8 * np.log(every)      # exp() of it times 1 / every: an fp32 number
+    lp = (-3 * rng.random(n)).astype(np.float32)
+    near = lambda s: (lp + s * rng.standard_normal(n)).astype(np.float32)      # noqa: E731
+    adv = -1 - rng.random(n).astype(np.float32)      # not clipped from above
+    for what, scale in (("ratio", 1.0), ("kl", 1.0), ("scale", 1e37)):
+        old, ref = near(0.2), near(0.2)
+        at = 1 + int(rng.integers(0, every - 5))
+        if what == "ratio":
+            old[at:at + 5] = lp[at:at + 5] - np.float32(top - 1)
+        elif what == "kl":
+            ref[at:at + 5] = lp[at:at + 5] + np.float32(top)
+        else:
+            adv[at:at + 5] *= 60
+        got = run_policy(lp, old, ref, adv, None, off, kl=0.05, by_seq=by_seq, per_token=True, grad_scale=scale)
+        want = T.policy(lp, old, ref, adv, None, off, f32(0.2), f32(0.28), f32(0.05), by_seq, True, f32(scale))
+        most = np.abs(want["dlogp"]).max()
+        assert most < 3.3e38 < most * every, what
+        assert np.isfinite(got["dlogp"]).all() and (np.abs(got["dlogp"] - want["dlogp"]) <= TOL * want["size"]).all(), what
+        size = max(want["size"].max() / scale * every, 1.0)
+        if abs(want["loss"]) < 3e38:
+            assert abs(got["loss"][0] - want["loss"]) <= TOL * max(size, abs(want["loss"]))
+        if want["kl"] < 3e38:
+            assert abs(got["kl"][0] - want["kl"]) <= 101 * TOL * want["kl"]
