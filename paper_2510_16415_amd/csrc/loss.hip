@@ -31,6 +31,13 @@ constexpr int kSmallTokens = 512, kSmallSeqs = 16;
 
 constexpr int kClearTokens = 16384;
 
+// Batches of more sequences have their counts and sums added up by a launch in between: every workgroup of the second launch needs
+// the count over all, and reading all counts there is quadratic in the sequences.  Without / with that launch, means over tokens, over
+// sequences, us: 1800 sequences of 8 tokens 18, 21 / 22, 22; 3000 25, 31 / 24, 25; 8192 60, 82 / 42, 43; 32768 358, 578 / 124, 132; with it
+// 1048576 3790, 4040.
+constexpr int kGatherFrom = 2048;
+constexpr int kGathered = 256;       // workgroups of that launch at most
+
 struct Part { double sum; double count; };
 
 __device__ inline TokenRange sequence(const int64_t* offsets, int64_t tokens, int k) { return token_range(offsets[k], offsets[k + 1], tokens); }
@@ -246,6 +253,8 @@ struct PolicyArgs {
   float *loss, *kl, *clipped, *dlogp;
   double* sums;         // [3][sequences * slices]: loss, KL, clipped tokens
   uint32_t* counts;     // [sequences][slices]: counted tokens
+  double* gathered;     // [4][groups]: of a range of sequences the count for the weights; loss, KL, clipped tokens without the common part of their weights
+  int groups;           // 0: nothing is gathered
   int64_t tokens;
   int seqs, slices, by_sequence, per_token;
   double low, high, log_low, log_high;      // bounds of the ratio, and their logarithms
@@ -385,6 +394,21 @@ __global__ __launch_bounds__(kThreads) void policy_tokens_kernel(const PolicyArg
   a.counts[blockIdx.x] = (uint32_t)t[3];
 }
 
+// Between the two where there are many sequences, which are short then: a slice each.  A workgroup adds up a range of them, a thread to a sequence.
+__global__ __launch_bounds__(kThreads) void policy_gather_kernel(const PolicyArgs a) {
+  const int per = (a.seqs + a.groups - 1) / a.groups, lo = blockIdx.x * per, hi = min(lo + per, a.seqs);
+  double t[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 2
+  for (int i = lo + threadIdx.x; i < hi; i += kThreads) {
+    const double own = a.counts[i], w = a.by_sequence ? (own > 0.0 ? 1.0 / own : 0.0) : 1.0;
+    t[0] += share(a, own);
+    for (int m = 0; m < 3; ++m) t[m + 1] += a.sums[(int64_t)m * a.seqs + i] * w;
+  }
+  block_sums(t);
+  if (threadIdx.x == 0)
+    for (int m = 0; m < 4; ++m) a.gathered[m * a.groups + blockIdx.x] = t[m];
+}
+
 // Workgroup seqs * slices: the results; those behind it: the tokens of no sequence.  Sequences of many slices are added up by 16
 // lanes each, where there are no more than four by a wave each (means over sequences, us, a wave each / this: 64 sequences of 16000 tokens 41.5 / 22.5, 16 of
 // 60000 23.4 / 18.4, 2 of 200000 15.2 / 13.5).
@@ -412,7 +436,9 @@ __global__ __launch_bounds__(kThreads) void policy_scale_kernel(const PolicyArgs
   // all counted tokens, or the sequences that have any
   auto all = [&]() {
     double n = 0.0;
-    if (!a.by_sequence) {
+    if (a.groups > 0) {
+      if ((int)threadIdx.x < a.groups) n = a.gathered[threadIdx.x];
+    } else if (!a.by_sequence) {
       for (int i = threadIdx.x; i < grads; i += kThreads) n += a.counts[i];
     } else if (rows) {
       auto live = [&](auto of) {
@@ -435,7 +461,11 @@ __global__ __launch_bounds__(kThreads) void policy_scale_kernel(const PolicyArgs
   auto add = [&](int q, double w) {
     for (int m = 0; m < 3; ++m) t[m] += a.sums[(int64_t)m * grads + q] * w;
   };
-  if (!a.by_sequence) {
+  if (a.groups > 0) {
+    const double w = token_weight(a, n, 1.0);
+    if ((int)threadIdx.x < a.groups)
+      for (int m = 0; m < 3; ++m) t[m] = a.gathered[(m + 1) * a.groups + threadIdx.x] * w;
+  } else if (!a.by_sequence) {
     const double w = token_weight(a, n, 0.0);
 #pragma unroll 2
     for (int q = threadIdx.x; q < grads; q += kThreads) add(q, w);
@@ -536,7 +566,17 @@ void* aligned(void* ws) { return (void*)(((uintptr_t)ws + 255) / 256 * 256); }
 size_t preference_bytes(const mecefo_preference_desc_t* d) {
   return (size_t)2 * d->pairs * slices_of(d->tokens, (int64_t)d->pairs * 2) * sizeof(Part) + 256;
 }
-size_t policy_bytes(const mecefo_policy_desc_t* d) { return (size_t)d->sequences * slices_of(d->tokens, d->sequences) * (3 * sizeof(double) + sizeof(uint32_t)) + 256; }
+// Workgroups of the launch that gathers, 0 where there is none.  Sequences are one slice each there: with 4 * kCUs of them or more the
+// mean is no longer than a slice.
+int groups_of(int64_t sequences) {
+  static_assert(kGatherFrom >= 4 * kCUs && kGathered <= kThreads, "");
+  const int64_t n = (sequences + kThreads - 1) / kThreads;
+  return sequences <= kGatherFrom ? 0 : (int)(n < kGathered ? n : kGathered);
+}
+size_t policy_bytes(const mecefo_policy_desc_t* d) {
+  return (size_t)d->sequences * slices_of(d->tokens, d->sequences) * (3 * sizeof(double) + sizeof(uint32_t)) +
+         4 * groups_of(d->sequences) * sizeof(double) + 256;
+}
 
 }  // namespace
 }  // namespace mecefo
@@ -604,8 +644,10 @@ mecefo_status_t mecefo_policy_loss(const mecefo_policy_desc_t* desc, const float
   TRY(check_ws(policy_bytes(desc), ws, ws_bytes));
   hipStream_t s = (hipStream_t)hip_stream;
   const int slices = slices_of(desc->tokens, desc->sequences), grads = desc->sequences * slices;
-  const PolicyArgs a = {logp, old_logp, ref_logp, advantage, mask, offsets, loss, kl, clipped, dlogp, (double*)aligned(ws),
-                        (uint32_t*)((double*)aligned(ws) + (int64_t)3 * grads), desc->tokens, desc->sequences, slices, desc->mean == MECEFO_MEAN_SEQUENCES, desc->advantage_per_token,
+  const int groups = groups_of(desc->sequences);
+  double* const sums = (double*)aligned(ws) + 4 * groups;      // what is gathered lies in front of it
+  const PolicyArgs a = {logp, old_logp, ref_logp, advantage, mask, offsets, loss, kl, clipped, dlogp, sums,
+                        (uint32_t*)(sums + (int64_t)3 * grads), (double*)aligned(ws), groups, desc->tokens, desc->sequences, slices, desc->mean == MECEFO_MEAN_SEQUENCES, desc->advantage_per_token,
                         1.0 - (double)desc->clip_low, 1.0 + (double)desc->clip_high, log1p(-(double)desc->clip_low),
                         log1p((double)desc->clip_high), desc->kl_coef, desc->grad_scale};
   if (small(desc->tokens, desc->sequences)) {
@@ -615,6 +657,10 @@ mecefo_status_t mecefo_policy_loss(const mecefo_policy_desc_t* desc, const float
   }
   if (grads > 0) {
     hipLaunchKernelGGL(policy_tokens_kernel, dim3(grads), dim3(kThreads), 0, s, a);
+    LAUNCHED("policy_loss");
+  }
+  if (groups > 0) {
+    hipLaunchKernelGGL(policy_gather_kernel, dim3(groups), dim3(kThreads), 0, s, a);
     LAUNCHED("policy_loss");
   }
   hipLaunchKernelGGL(policy_scale_kernel, dim3(grads + 1 + clears(desc->tokens)), dim3(kThreads), 0, s, a);
