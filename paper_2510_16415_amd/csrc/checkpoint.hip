@@ -310,7 +310,9 @@ mecefo_status_t check_call(mecefo_dtype_t dtype, const void* X, int64_t rows, in
   const int ck = check_ckpt(ckpt, rows, cols, "ckpt", k);
   if (ck != MECEFO_OK) return (mecefo_status_t)ck;
   const uintptr_t x = (uintptr_t)X, q = (uintptr_t)k->q, e = (uintptr_t)k->e;
-  const uintptr_t nx = rows * ldx * (bf16 ? 2 : 4), nq = rows * k->ldq, ne = rows * k->lde;
+  // from the first element to the last: what lies behind a last row's columns may belong to another tensor
+  const int64_t groups = ((int64_t)cols + 31) / 32;
+  const uintptr_t nx = ((rows - 1) * ldx + cols) * (bf16 ? 2 : 4), nq = (rows - 1) * k->ldq + 32 * groups, ne = (rows - 1) * k->lde + groups;
   if (rows > 0 && ((x < q + nq && q < x + nx) || (x < e + ne && e < x + nx) || (q < e + ne && e < q + nq)))
     return (mecefo_status_t)fail(MECEFO_ERR_INVALID_ARG, "the tensor and the parts of its checkpoint overlap");
   return MECEFO_OK;
