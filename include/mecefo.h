@@ -442,8 +442,9 @@ mecefo_status_t mecefo_head_logprob_bwd(const mecefo_head_desc_t* desc, const vo
  * [offsets[k], offsets[k + 1]) of the token arrays (offsets: device memory, not decreasing, within [0, tokens]; a sequence may
  * be empty; offsets that break this give undefined results, but nothing outside the arrays is touched).  mask [tokens]: a token
  * with 0 is not counted, and what the arrays hold for it is not used; NULL counts all.  dlogp [tokens] is written
- * as a whole: zero for what is not counted or belongs to no sequence; no output may overlap an input.  Sums are taken in fp64, in an order that depends on
- * the sizes only.  All values fp32, at most 2^20 sequences. */
+ * as a whole: zero for what is not counted or belongs to no sequence; outputs and the workspace must not overlap each other or an
+ * input (MECEFO_ERR_INVALID_ARG).  Sums are taken in fp64, in an order that depends on the sizes only.  All values fp32, at most
+ * 2^20 sequences. */
 
 /* Preference loss over pairs; sequence 2i is the preferred answer of pair i, sequence 2i + 1 the other one.
  *   r_k = beta * sum over the counted tokens of (logp - ref_logp), or beta times their mean (length_mean; 0 for none);

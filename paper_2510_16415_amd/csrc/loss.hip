@@ -561,6 +561,18 @@ mecefo_status_t check_ws(size_t need, const void* ws, size_t ws_bytes) {
   if (!ws) return (mecefo_status_t)fail(MECEFO_ERR_INVALID_ARG, "workspace is NULL");
   return MECEFO_OK;
 }
+// What a call writes, the workspace among it, lies apart from everything else that it gets.
+struct Span { const void* p; size_t bytes; const char* name; bool written; };
+template <size_t N>
+mecefo_status_t check_apart(const Span (&v)[N]) {
+  for (size_t i = 0; i < N; ++i)
+    for (size_t j = 0; j < N; ++j) {
+      if (!v[i].written || i == j || !v[i].p || !v[j].p || !v[i].bytes || !v[j].bytes) continue;
+      const uintptr_t x = (uintptr_t)v[i].p, y = (uintptr_t)v[j].p;
+      if (x < y + v[j].bytes && y < x + v[i].bytes) return (mecefo_status_t)fail(MECEFO_ERR_INVALID_ARG, "%s overlaps %s", v[i].name, v[j].name);
+    }
+  return MECEFO_OK;
+}
 void* aligned(void* ws) { return (void*)(((uintptr_t)ws + 255) / 256 * 256); }
 
 size_t preference_bytes(const mecefo_preference_desc_t* d) {
@@ -605,6 +617,12 @@ mecefo_status_t mecefo_preference_loss(const mecefo_preference_desc_t* desc, con
   TRY(check_align(margins, "margins", 4, false)); TRY(check_align(rewards, "rewards", 4, false));
   TRY(check_align(dlogp, "dlogp", 4, any));
   TRY(check_ws(preference_bytes(desc), ws, ws_bytes));
+  const size_t tokens = (size_t)desc->tokens, pairs = (size_t)desc->pairs;
+  const Span spans[] = {{loss, 4, "loss", true}, {margins, 4 * pairs, "margins", true}, {rewards, 8 * pairs, "rewards", true},
+                        {dlogp, 4 * tokens, "dlogp", true}, {ws, preference_bytes(desc), "the workspace", true},
+                        {logp, 4 * tokens, "logp", false}, {ref_logp, 4 * tokens, "ref_logp", false}, {mask, tokens, "mask", false},
+                        {offsets, pairs > 0 ? 8 * (2 * pairs + 1) : 0, "offsets", false}};
+  TRY(check_apart(spans));
   hipStream_t s = (hipStream_t)hip_stream;
   const int slices = slices_of(desc->tokens, (int64_t)desc->pairs * 2), grads = 2 * desc->pairs * slices;
   const PrefArgs a = {logp, ref_logp, mask, offsets, loss, margins, rewards, dlogp, (Part*)aligned(ws), desc->tokens, desc->pairs,
@@ -642,6 +660,13 @@ mecefo_status_t mecefo_policy_loss(const mecefo_policy_desc_t* desc, const float
   TRY(check_align(dlogp, "dlogp", 4, any));
   if (!ref_logp && desc->kl_coef != 0.f) return (mecefo_status_t)fail(MECEFO_ERR_INVALID_ARG, "kl_coef needs ref_logp");
   TRY(check_ws(policy_bytes(desc), ws, ws_bytes));
+  const size_t tokens = (size_t)desc->tokens, seqs = (size_t)desc->sequences;
+  const Span spans[] = {{loss, 4, "loss", true}, {kl, 4, "kl", true}, {clipped, 4, "clipped", true}, {dlogp, 4 * tokens, "dlogp", true},
+                        {ws, policy_bytes(desc), "the workspace", true}, {logp, 4 * tokens, "logp", false},
+                        {old_logp, 4 * tokens, "old_logp", false}, {ref_logp, 4 * tokens, "ref_logp", false},
+                        {advantage, 4 * (desc->advantage_per_token ? tokens : seqs), "advantage", false}, {mask, tokens, "mask", false},
+                        {offsets, seqs > 0 ? 8 * (seqs + 1) : 0, "offsets", false}};
+  TRY(check_apart(spans));
   hipStream_t s = (hipStream_t)hip_stream;
   const int slices = slices_of(desc->tokens, desc->sequences), grads = desc->sequences * slices;
   const int groups = groups_of(desc->sequences);
