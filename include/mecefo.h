@@ -366,7 +366,8 @@ mecefo_status_t mecefo_block_bwd_skip_ex(const mecefo_ffn_desc_t* desc, const vo
  * A group that holds an infinity or a NaN is stored as e = 255 and q = 0 and stands for NaN in all its columns.
  * Every value that a checkpoint stands for is a bf16 number: unpacking is exact in either dtype.
  * q [rows x ld_q]: 16-byte aligned, ld_q a multiple of 16 and >= 32 ceil(cols / 32); the columns behind cols are written as
- * zeros.  e [rows x ld_e]: ld_e >= ceil(cols / 32).  Both below 2 GiB.  No part may overlap the tensor. */
+ * zeros.  e [rows x ld_e]: ld_e >= ceil(cols / 32).  Both below 2 GiB.  The tensor, q and e must not overlap, each from its
+ * first element to its last; nor may what a call below writes (X_out, dX, dX_bottom, the workspace) overlap a checkpoint. */
 typedef struct {
   void* q;
   void* e;

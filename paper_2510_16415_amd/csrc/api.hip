@@ -727,6 +727,15 @@ mecefo_status_t check_lowrank_args(const Ctx& c, const mecefo_proj_t P[3], mecef
 struct KeptCkpts { const mecefo_ckpt_t *H, *G, *Z; };
 // Room behind the workspace of the backward for the values of H.
 size_t kept_bytes(const Ctx& c) { return (size_t)up(c.b * c.dm * c.esz, 256); }
+// A checkpoint lies apart from what the call writes: `bytes` at `out`.
+mecefo_status_t check_clear(const Ctx& c, const Ckpt& k, int cols, const char* name, const void* out, size_t bytes, const char* out_name) {
+  if (c.b == 0 || !k.q || !out) return MECEFO_OK;
+  const uintptr_t o = (uintptr_t)out, q = (uintptr_t)k.q, e = (uintptr_t)k.e;
+  const uintptr_t groups = cdiv(cols, kCkptGroup), nq = (c.b - 1) * k.ldq + kCkptGroup * groups, ne = (c.b - 1) * k.lde + groups;
+  if ((o < q + nq && q < o + bytes) || (o < e + ne && e < o + bytes))
+    return fail(MECEFO_ERR_INVALID_ARG, "%s overlaps checkpoint %s", out_name, name);
+  return MECEFO_OK;
+}
 
 // The neighbor-mode backward behind its entry points.  kept: the stored tensors as 8-bit checkpoints, which are unpacked
 // into the workspace (H, opt->G and opt->Z are then NULL), or NULL.
@@ -768,6 +777,14 @@ mecefo_status_t block_bwd_skip(const mecefo_ffn_desc_t* desc, const void* H, con
   TRY(carve(c, r, side, ws, ws_bytes, &bf, kept ? kept_bytes(c) : 0));
   hipStream_t s = (hipStream_t)hip_stream;
   char* base = bf.base;
+  if (kept) {
+    const Ckpt* k[3] = {&kh, &kg, &kz};
+    const char* const name[3] = {"H", "G", "Z"};
+    for (int i = 0; i < 3; ++i) {
+      TRY(check_clear(c, *k[i], i ? c.ff : c.dm, name[i], dX, act_span(c, desc->ld_act_d), "dX"));
+      TRY(check_clear(c, *k[i], i ? c.ff : c.dm, name[i], base, bf.w.end + kept_bytes(c), "the workspace"));
+    }
+  }
   int64_t ldh = desc->ld_act_d;
   const bool unpack = kept && c.b > 0;
   if (unpack) {
@@ -1433,9 +1450,15 @@ mecefo_status_t block_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_
 }
 
 // ---- stacks ---------------------------------------------------------------------------------
-mecefo_status_t check_ckpts(const Ctx& c, const mecefo_ckpt_t* kept, int n_layers) {
+// out: the activation [b x d] that the call leaves; need: bytes of the workspace that it takes.
+mecefo_status_t check_ckpts(const Ctx& c, const mecefo_ckpt_t* kept, int n_layers, const void* out, const char* out_name, const void* ws,
+                            size_t need) {
   Ckpt k;
-  for (int l = 0; l < n_layers; ++l) TRY((mecefo_status_t)check_ckpt(&kept[l], c.b, c.dm, "H", &k));
+  for (int l = 0; l < n_layers; ++l) {
+    TRY((mecefo_status_t)check_ckpt(&kept[l], c.b, c.dm, "H", &k));
+    TRY(check_clear(c, k, c.dm, "H", out, act_span(c, c.d->ld_act_d), out_name));
+    TRY(check_clear(c, k, c.dm, "H", ws, need, "the workspace"));
+  }
   return MECEFO_OK;
 }
 
@@ -1448,11 +1471,11 @@ mecefo_status_t stack_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_
   TRY(check_attn(c, attn));
   if (n_layers < 1) return fail(MECEFO_ERR_INVALID_ARG, "n_layers must be >= 1");
   if (!layers || (!H && !kept)) return fail(MECEFO_ERR_INVALID_ARG, "layers and H are required");
-  if (kept) TRY(check_ckpts(c, kept, n_layers));
-  if (c.b > 0 && X_out == X0) return fail(MECEFO_ERR_INVALID_ARG, "X_out must not alias X0");
   const FwdWs plan = fwd_layout(c, *attn);
   const size_t inner = plan.total;
   const size_t act = (size_t)up(c.b * desc->ld_act_d * c.esz, 256);
+  if (kept) TRY(check_ckpts(c, kept, n_layers, X_out, "X_out", ws, 3 * act + inner));
+  if (c.b > 0 && X_out == X0) return fail(MECEFO_ERR_INVALID_ARG, "X_out must not alias X0");
   if (!ws) return fail(MECEFO_ERR_INVALID_ARG, "workspace is NULL");
   char* base = (char*)up((int64_t)(uintptr_t)ws, 256);
   const size_t lead = (size_t)(base - (char*)ws);
@@ -1546,7 +1569,13 @@ mecefo_status_t mecefo_stack_bwd_skip_ckpt(const mecefo_ffn_desc_t* desc, int n_
   if (!layers || !H || !lowrank) return fail(MECEFO_ERR_INVALID_ARG, "layers, H and lowrank are required");
   Ctx c;
   TRY(check_desc(desc, &c));
-  TRY(check_ckpts(c, H, n_layers));
+  size_t need = 0;      // of the layer that takes the most
+  for (int l = 0; l < n_layers; ++l) {
+    const int r[3] = {lowrank[l].Pg.r, lowrank[l].Pu.r, lowrank[l].Pd.r};
+    const size_t n = layout(c, r, side, 0, true).total + kept_bytes(c);
+    need = n > need ? n : need;
+  }
+  TRY(check_ckpts(c, H, n_layers, dX_bottom, "dX_bottom", ws, need < ws_bytes ? need : ws_bytes));
   const void* g = dOut_top;
   for (int l = n_layers - 1; l >= 0; --l) {
     const mecefo_layer_weights_t& w = layers[l];

@@ -55,3 +55,56 @@ def test_the_losses_workspaces(name):
         d = B.make_preference_desc(TOKENS, SEQS // 2)
         need = B.mecefo_preference_workspace_bytes(d)
         overlaps(B.mecefo_preference_loss, d, PREFERENCE, need, {name: 16384})
+
+
+def kept(q=None, e=None, cols=32):
+    """A checkpoint of 2 rows, far from the other arguments where nothing else is said."""
+    g = -(-cols // 32)
+    base = at().data_ptr()
+    return B.Ckpt(base + (q if q is not None else 57344 + 1024 * g), base + (e if e is not None else 61440 + 64 * g), 32 * g + 16, g + 1)
+
+
+BLOCK = B.make_desc(2, 32, 64, B.BF16, ld_act_d=40)
+DX, WS = 12288, 32768      # dX: 2 rows of stride 40, 144 bytes from the first element to the last
+
+
+def block(**k):
+    need = B.mecefo_block_ckpt_workspace_bytes(BLOCK)
+    a = dict(desc=BLOCK, H=kept(), dOut=at(512), gamma=at(1024), Wg=at(2048), Wu=at(2048), Wd=at(2048), Pg=None, Pu=None, Pd=None,
+             side=B.SIDE_INPUT, dX=at(DX), dgamma=at(14336), dWg=at(16384), dWu=at(20480), dWd=at(28672), accumulate=0,
+             ws=at(WS)[:need], G=None, Z=None, exact_wgrad_mask=7, stream=STREAM)
+    a.update(k)
+    assert WS + need < 57344
+    return a
+
+
+@pytest.mark.parametrize("place", [DX, DX + 128, DX - 48])
+@pytest.mark.parametrize("name", ["H", "G", "Z"])
+def test_dx_over_a_checkpoint(name, place):
+    cols = 32 if name == "H" else 64
+    both = {} if name == "H" else dict(G=kept(cols=64), Z=kept(cols=64, q=60160, e=63488))
+    both[name] = kept(cols=cols, q=place)
+    refused(INV, f"dX overlaps checkpoint {name}", B.mecefo_block_bwd_skip_ckpt, **block(**both))
+    both[name] = kept(cols=cols, e=place + 14 if place == DX + 128 else max(place, DX - 1))
+    refused(INV, f"dX overlaps checkpoint {name}", B.mecefo_block_bwd_skip_ckpt, **block(**both))
+
+
+@pytest.mark.parametrize("name", ["H", "G", "Z"])
+def test_a_workspace_over_a_checkpoint(name):
+    need = B.mecefo_block_ckpt_workspace_bytes(BLOCK) - 256      # the rest is for the alignment of the base
+    for place in (WS, WS + need - 16):
+        both = {} if name == "H" else dict(G=kept(cols=64), Z=kept(cols=64, q=60160, e=63488))
+        both[name] = kept(cols=32 if name == "H" else 64, q=place)
+        refused(INV, f"the workspace overlaps checkpoint {name}", B.mecefo_block_bwd_skip_ckpt, **block(**both))
+
+
+def test_stacks_over_the_checkpoints_of_any_layer():
+    d, a = B.make_desc(2, 32, 64, B.BF16), B.make_attn_desc(1, 2, 1, 32)
+    need = B.mecefo_stack_ckpt_workspace_bytes(d, a)
+    assert WS + need < 57344
+    layers, low, ws = B.layer_weights([{}, {}]), (B.LayerLowrank * 2)(), at(WS)[:need]
+    for bad, text in ((kept(q=512), "overlaps checkpoint H"), (kept(e=512 + 127), "overlaps checkpoint H"), (kept(q=WS + 1024), "the workspace overlaps")):
+        for ks in ([bad, kept(q=60000 // 16 * 16)], [kept(q=60000 // 16 * 16), bad]):
+            ks = B.ckpt_array(ks)
+            refused(INV, text, B.mecefo_stack_fwd_neighbor_ckpt, d, a, layers, at(), ks, at(512), ws, STREAM)
+            refused(INV, text, B.mecefo_stack_bwd_skip_ckpt, d, layers, ks, low, B.SIDE_INPUT, at(), at(512), 0, ws, STREAM)
