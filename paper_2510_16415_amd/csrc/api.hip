@@ -708,11 +708,11 @@ FwdWs fwd_layout(const Ctx& c, const mecefo_attn_desc_t& a) {
 
 // The block forward behind mecefo_block_fwd.  plan: the layout that every layer of one public call shares, NULL to
 // make it here; tables_ready: the workspace holds the rotary tables of a previous layer of the same plan; ckpt: where H
-// goes as an 8-bit checkpoint besides.
+// goes as an 8-bit checkpoint besides; check_only: nothing is enqueued.
 mecefo_status_t block_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn,
                           const mecefo_block_fwd_inputs_t* in, const mecefo_block_fwd_outputs_t* out,
                           const FwdWs* plan, void* ws, size_t ws_bytes, void* hip_stream, bool tables_ready,
-                          const Ckpt* ckpt = nullptr);
+                          const Ckpt* ckpt = nullptr, bool check_only = false);
 
 mecefo_status_t check_lowrank_args(const Ctx& c, const mecefo_proj_t P[3], mecefo_side_t side, int exact_mask = 0) {
   if (side != MECEFO_SIDE_INPUT && side != MECEFO_SIDE_OUTPUT) return fail(MECEFO_ERR_INVALID_ARG, "side must be MECEFO_SIDE_INPUT or MECEFO_SIDE_OUTPUT");
@@ -738,13 +738,13 @@ mecefo_status_t check_clear(const Ctx& c, const Ckpt& k, int cols, const char* n
 }
 
 // The neighbor-mode backward behind its entry points.  kept: the stored tensors as 8-bit checkpoints, which are unpacked
-// into the workspace (H, opt->G and opt->Z are then NULL), or NULL.
+// into the workspace (H, opt->G and opt->Z are then NULL), or NULL.  check_only: nothing is enqueued.
 mecefo_status_t block_bwd_skip(const mecefo_ffn_desc_t* desc, const void* H, const KeptCkpts* kept, const void* dOut,
                                const void* gamma, const void* Wg, const void* Wu, const void* Wd,
                                mecefo_proj_t Pg, mecefo_proj_t Pu, mecefo_proj_t Pd, mecefo_side_t side,
                                const mecefo_skip_options_t* opt, void* dX, void* dgamma, void* dWg,
                                void* dWu, void* dWd, int accumulate, void* ws, size_t ws_bytes,
-                               void* hip_stream) {
+                               void* hip_stream, bool check_only = false) {
   Ctx c;
   TRY(check_desc(desc, &c));
   const void* Gs = opt ? opt->G : nullptr;
@@ -785,6 +785,7 @@ mecefo_status_t block_bwd_skip(const mecefo_ffn_desc_t* desc, const void* H, con
       TRY(check_clear(c, *k[i], i ? c.ff : c.dm, name[i], base, bf.w.end + kept_bytes(c), "the workspace"));
     }
   }
+  if (check_only) return MECEFO_OK;
   int64_t ldh = desc->ld_act_d;
   const bool unpack = kept && c.b > 0;
   if (unpack) {
@@ -1338,7 +1339,7 @@ namespace {
 mecefo_status_t block_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn,
                           const mecefo_block_fwd_inputs_t* in, const mecefo_block_fwd_outputs_t* out,
                           const FwdWs* plan, void* ws, size_t ws_bytes, void* hip_stream, bool tables_ready,
-                          const Ckpt* ckpt) {
+                          const Ckpt* ckpt, bool check_only) {
   Ctx c;
   TRY(check_desc(desc, &c));
   TRY(check_attn(c, attn));
@@ -1356,7 +1357,7 @@ mecefo_status_t block_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_
   const FwdWs w = plan ? *plan : fwd_layout(c, *attn);
   if (w.total > ws_bytes) return fail(MECEFO_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, w.total);
   if (!ws) return fail(MECEFO_ERR_INVALID_ARG, "workspace is NULL");
-  if (!any) return MECEFO_OK;
+  if (!any || check_only) return MECEFO_OK;
   char* base = (char*)up((int64_t)(uintptr_t)ws, 256);
   hipStream_t s = (hipStream_t)hip_stream;
   const mecefo_ffn_desc_t& d = *desc;
@@ -1462,6 +1463,27 @@ mecefo_status_t check_ckpts(const Ctx& c, const mecefo_ckpt_t* kept, int n_layer
   return MECEFO_OK;
 }
 
+// The backward behind its two entry points.  The gradient travels down in dX_bottom's buffer: every layer overwrites its dOut
+// with its dX.
+mecefo_status_t stack_bwd(const mecefo_ffn_desc_t* desc, int n_layers, const mecefo_layer_weights_t* layers, const void* const* H,
+                          const mecefo_ckpt_t* kept, const mecefo_layer_lowrank_t* lowrank, mecefo_side_t side, const void* dOut_top,
+                          void* dX_bottom, int accumulate, void* ws, size_t ws_bytes, void* hip_stream) {
+  auto pass = [&](bool check_only) -> mecefo_status_t {
+    const void* g = dOut_top;
+    for (int l = n_layers - 1; l >= 0; --l) {
+      const mecefo_layer_weights_t& w = layers[l];
+      const mecefo_layer_lowrank_t& q = lowrank[l];
+      const KeptCkpts k = {kept ? &kept[l] : nullptr, nullptr, nullptr};
+      TRY(block_bwd_skip(desc, kept ? nullptr : H[l], kept ? &k : nullptr, g, w.g_ffn, w.Wg, w.Wu, w.Wd, q.Pg, q.Pu, q.Pd, side, nullptr,
+                         dX_bottom, q.dg_ffn, q.dWg, q.dWu, q.dWd, accumulate, ws, ws_bytes, hip_stream, check_only));
+      g = dX_bottom;
+    }
+    return MECEFO_OK;
+  };
+  TRY(pass(true));
+  return pass(false);
+}
+
 // The forward behind its two entry points: every layer's H stays as it is, or is kept as an 8-bit checkpoint.
 mecefo_status_t stack_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn, int n_layers,
                           const mecefo_layer_weights_t* layers, const void* X0, void* const* H, const mecefo_ckpt_t* kept,
@@ -1483,20 +1505,23 @@ mecefo_status_t stack_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_
   if (front + inner > ws_bytes) return fail(MECEFO_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, front + inner);
   void* pp[2] = {base, base + act};
   void* inner_ws = (char*)ws + front;
-  const void* x = X0;
-  for (int l = 0; l < n_layers; ++l) {
-    const mecefo_layer_weights_t& w = layers[l];
-    mecefo_block_fwd_inputs_t in = {x, w.g_attn, w.g_ffn, w.Wq, w.Wk, w.Wv, w.Wo, w.Wg, w.Wu, w.Wd};
-    void* y = l == n_layers - 1 ? X_out : pp[l & 1];
-    mecefo_block_fwd_outputs_t out = {y, kept ? base + 2 * act : H[l], nullptr, nullptr, nullptr, nullptr, nullptr};
-    // every layer of the call uses the same workspace and layout: the angle tables of the first one serve them all
-    Ckpt k;
-    if (kept) TRY((mecefo_status_t)check_ckpt(&kept[l], c.b, c.dm, "H", &k));
-    mecefo_status_t st = block_fwd(desc, attn, &in, &out, &plan, inner_ws, ws_bytes - front, hip_stream, l > 0, kept ? &k : nullptr);
-    if (st != MECEFO_OK) return st;
-    x = y;
-  }
-  return MECEFO_OK;
+  auto pass = [&](bool check_only) -> mecefo_status_t {
+    const void* x = X0;
+    for (int l = 0; l < n_layers; ++l) {
+      const mecefo_layer_weights_t& w = layers[l];
+      mecefo_block_fwd_inputs_t in = {x, w.g_attn, w.g_ffn, w.Wq, w.Wk, w.Wv, w.Wo, w.Wg, w.Wu, w.Wd};
+      void* y = l == n_layers - 1 ? X_out : pp[l & 1];
+      mecefo_block_fwd_outputs_t out = {y, kept ? base + 2 * act : H[l], nullptr, nullptr, nullptr, nullptr, nullptr};
+      Ckpt k;
+      if (kept) TRY((mecefo_status_t)check_ckpt(&kept[l], c.b, c.dm, "H", &k));
+      // every layer of the call uses the same workspace and layout: the angle tables of the first one serve them all
+      TRY(block_fwd(desc, attn, &in, &out, &plan, inner_ws, ws_bytes - front, hip_stream, l > 0, kept ? &k : nullptr, check_only));
+      x = y;
+    }
+    return MECEFO_OK;
+  };
+  TRY(pass(true));
+  return pass(false);
 }
 }  // namespace
 
@@ -1527,18 +1552,7 @@ mecefo_status_t mecefo_stack_bwd_skip(const mecefo_ffn_desc_t* desc, int n_layer
                                       size_t ws_bytes, void* hip_stream) {
   if (n_layers < 1) return fail(MECEFO_ERR_INVALID_ARG, "n_layers must be >= 1");
   if (!layers || !H || !lowrank) return fail(MECEFO_ERR_INVALID_ARG, "layers, H and lowrank are required");
-  // the gradient travels down in dX_bottom's buffer: every layer overwrites its dOut with its dX
-  const void* g = dOut_top;
-  for (int l = n_layers - 1; l >= 0; --l) {
-    const mecefo_layer_weights_t& w = layers[l];
-    const mecefo_layer_lowrank_t& q = lowrank[l];
-    mecefo_status_t st = mecefo_block_bwd_skip(desc, H[l], g, w.g_ffn, w.Wg, w.Wu, w.Wd, q.Pg, q.Pu, q.Pd, side,
-                                               dX_bottom, q.dg_ffn, q.dWg, q.dWu, q.dWd, accumulate, ws, ws_bytes,
-                                               hip_stream);
-    if (st != MECEFO_OK) return st;
-    g = dX_bottom;
-  }
-  return MECEFO_OK;
+  return stack_bwd(desc, n_layers, layers, H, nullptr, lowrank, side, dOut_top, dX_bottom, accumulate, ws, ws_bytes, hip_stream);
 }
 
 mecefo_status_t mecefo_stack_ckpt_workspace_bytes(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn,
@@ -1576,15 +1590,7 @@ mecefo_status_t mecefo_stack_bwd_skip_ckpt(const mecefo_ffn_desc_t* desc, int n_
     need = n > need ? n : need;
   }
   TRY(check_ckpts(c, H, n_layers, dX_bottom, "dX_bottom", ws, need < ws_bytes ? need : ws_bytes));
-  const void* g = dOut_top;
-  for (int l = n_layers - 1; l >= 0; --l) {
-    const mecefo_layer_weights_t& w = layers[l];
-    const mecefo_layer_lowrank_t& q = lowrank[l];
-    TRY(mecefo_block_bwd_skip_ckpt(desc, &H[l], g, w.g_ffn, w.Wg, w.Wu, w.Wd, q.Pg, q.Pu, q.Pd, side, nullptr, nullptr, 0,
-                                   dX_bottom, q.dg_ffn, q.dWg, q.dWu, q.dWd, accumulate, ws, ws_bytes, hip_stream));
-    g = dX_bottom;
-  }
-  return MECEFO_OK;
+  return stack_bwd(desc, n_layers, layers, nullptr, H, lowrank, side, dOut_top, dX_bottom, accumulate, ws, ws_bytes, hip_stream);
 }
 
 mecefo_status_t mecefo_block_bwd_skip_noalloc(const mecefo_ffn_desc_t* desc, const void* H, const void* dOut,
