@@ -41,7 +41,8 @@
  * as 5461 needs ld >= 5464); columns between the logical width and the stride are
  * never read as data.  dtype MECEFO_F32: no alignment rule beyond 4 bytes.
  * Every tensor must be smaller than 2 GiB, counted from its first element to its last (an fp32
- * projection may span more).  With tokens == 0 the [b x *] pointers may be NULL.
+ * projection may span more).  Calls with a norm, and the LM head, take at most 2^26 - 64 tokens.  With tokens == 0 the [b x *]
+ * pointers may be NULL.
  *
  * Errors: argument checks happen on the host before anything is enqueued; on a
  * non-OK status nothing was launched by that call (MECEFO_ERR_LAUNCH excepted) and

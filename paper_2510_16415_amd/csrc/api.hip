@@ -101,6 +101,12 @@ mecefo_status_t check_ptr(const Ctx& c, const void* p, const char* name, bool re
   return MECEFO_OK;
 }
 
+// The norm kernels take a wave per row.
+mecefo_status_t check_norm_rows(const Ctx& c) {
+  if (c.b > kMaxWaveRows) return fail(MECEFO_ERR_UNSUPPORTED, "more than 2^26 - 64 tokens; split the token batch");
+  return MECEFO_OK;
+}
+
 // Bytes spanned by a [b x d_model] activation tensor with row stride ld.
 size_t act_span(const Ctx& c, int64_t ld) { return c.b > 0 ? (size_t)(((c.b - 1) * ld + c.dm) * c.esz) : 0; }
 
@@ -747,6 +753,7 @@ mecefo_status_t block_bwd_skip(const mecefo_ffn_desc_t* desc, const void* H, con
                                void* hip_stream, bool check_only = false) {
   Ctx c;
   TRY(check_desc(desc, &c));
+  if (gamma) TRY(check_norm_rows(c));
   const void* Gs = opt ? opt->G : nullptr;
   const void* Zs = opt ? opt->Z : nullptr;
   const int exact_mask = opt ? opt->exact_wgrad_mask : 0;
@@ -1117,6 +1124,7 @@ mecefo_status_t mecefo_block_bwd_full(const mecefo_ffn_desc_t* desc, const mecef
   Ctx c;
   TRY(check_desc(desc, &c));
   TRY(check_attn(c, attn));
+  TRY(check_norm_rows(c));
   if (!in || !out) return fail(MECEFO_ERR_INVALID_ARG, "input or output table is NULL");
   const bool any = c.b > 0;
   TRY(check_ptr(c, in->X, "X", any)); TRY(check_ptr(c, in->H, "H", any)); TRY(check_ptr(c, in->dOut, "dOut", any));
@@ -1343,6 +1351,7 @@ mecefo_status_t block_fwd(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_
   Ctx c;
   TRY(check_desc(desc, &c));
   TRY(check_attn(c, attn));
+  TRY(check_norm_rows(c));
   if (!in || !out) return fail(MECEFO_ERR_INVALID_ARG, "input or output table is NULL");
   const bool any = c.b > 0;
   TRY(check_ptr(c, in->X, "X", any));

@@ -15,42 +15,46 @@ namespace {
 
 __device__ inline bool counted(int64_t label, int vocab) { return label >= 0 && label < vocab; }
 
-// lse and logp of a row of fp32 products z (before logit_scale), a workgroup per row, in one pass with a running maximum.
-__global__ __launch_bounds__(1024) void head_rows_kernel(const float* __restrict__ Z, int64_t ldz, int vocab, float scale,
+// lse and logp of the rows of fp32 products z (before logit_scale), a workgroup per row, in one pass with a running maximum.
+constexpr int kRowGroups = 1 << 21;      // at most: a launch of 2^32 threads leaves some of them out, without an error
+__global__ __launch_bounds__(1024) void head_rows_kernel(const float* __restrict__ Z, int64_t ldz, int rows, int vocab, float scale,
                                                         const int64_t* __restrict__ labels, float* __restrict__ logp,
                                                         float* __restrict__ lse) {
   __shared__ float2 red[16];
-  const int64_t row = blockIdx.x;
-  const float* z = Z + row * ldz;
   auto join = [](float2 x, float2 y) {      // a share without columns is (-inf, 0)
     const float m = fmaxf(x.x, y.x), k = m == -INFINITY ? 0.f : m;
     return float2{m, x.y * expf(x.x - k) + y.y * expf(y.x - k)};
   };
-  float2 a = {-INFINITY, 0.f};
-  for (int v0 = 4 * threadIdx.x; v0 < vocab; v0 += 4096) {      // rows are whole vectors of eight
-    typedef __attribute__((ext_vector_type(4))) float f4;
-    const f4 x = *(const f4*)(z + v0);
-    float y[4], m = a.x;
+  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+    const float* z = Z + row * ldz;
+    float2 a = {-INFINITY, 0.f};
+    for (int v0 = 4 * threadIdx.x; v0 < vocab; v0 += 4096) {      // rows are whole vectors of eight
+      typedef __attribute__((ext_vector_type(4))) float f4;
+      const f4 x = *(const f4*)(z + v0);
+      float y[4], m = a.x;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      y[e] = v0 + e < vocab ? x[e] * scale : -INFINITY;
-      m = fmaxf(m, y[e]);
+      for (int e = 0; e < 4; ++e) {
+        y[e] = v0 + e < vocab ? x[e] * scale : -INFINITY;
+        m = fmaxf(m, y[e]);
+      }
+      float s = a.x == -INFINITY ? 0.f : a.y * expf(a.x - m);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s += expf(y[e] - m);
+      a = float2{m, s};
     }
-    float s = a.x == -INFINITY ? 0.f : a.y * expf(a.x - m);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s += expf(y[e] - m);
-    a = float2{m, s};
+    for (int o = 1; o < 64; o *= 2) a = join(a, float2{__shfl_xor(a.x, o, 64), __shfl_xor(a.y, o, 64)});
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 1; w < 16; ++w) a = join(a, red[w]);
+      const float l = a.x + logf(a.y);
+      const int64_t label = labels[row];
+      logp[row] = counted(label, vocab) ? z[label] * scale - l : 0.f;
+      if (lse) lse[row] = l;
+    }
+    if (row + gridDim.x < rows) __syncthreads();      // `red` is read
   }
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) a = join(a, float2{__shfl_xor(a.x, o, 64), __shfl_xor(a.y, o, 64)});
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-  for (int w = 1; w < 16; ++w) a = join(a, red[w]);
-  const float l = a.x + logf(a.y);
-  const int64_t label = labels[row];
-  logp[row] = counted(label, vocab) ? z[label] * scale - l : 0.f;
-  if (lse) lse[row] = l;
 }
 
 // lse and logp from the parts that the products' epilogue leaves: (largest z', sum of 2^(z' - that)) of a row over part_cols
@@ -214,6 +218,7 @@ mecefo_status_t check_desc(const mecefo_head_desc_t* d, bool backward, Head* h) 
   h->esz = h->bf16 ? 2 : 4;
   if (h->bf16 && d->d_model % 8) return FAIL(MECEFO_ERR_UNSUPPORTED, "bf16 path needs d_model to be a multiple of 8 (got %d)", d->d_model);
   if (h->bf16 && (d->ld_act_d % 8 || d->ld_w % 8)) return FAIL(MECEFO_ERR_INVALID_ARG, "bf16 path needs every row stride to be a multiple of 8 elements");
+  if (d->tokens > kMaxWaveRows) return FAIL(MECEFO_ERR_UNSUPPORTED, "more than 2^26 - 64 tokens; split the token batch");
   const bool parts = h->bf16 && !backward;
   if (reaches_2gib(d->tokens, d->ld_act_d, h->esz) || reaches_2gib(d->vocab, d->ld_w, h->esz) ||
       reaches_2gib(d->tokens, parts ? ((int64_t)d->vocab + 31) / 32 : up(d->vocab, 8), parts ? 8 : h->esz))
@@ -394,8 +399,8 @@ mecefo_status_t mecefo_head_logprob_fwd(const mecefo_head_desc_t* desc, const vo
     if (h.b >= 256) hipLaunchKernelGGL(head_parts_kernel<16>, dim3(cdiv(h.b, 16)), dim3(1024), 0, s, part, parts, h.b, h.vocab, zl, labels, logp, lse);
     else hipLaunchKernelGGL(head_parts_kernel<2>, dim3(cdiv(h.b, 2)), dim3(1024), 0, s, part, parts, h.b, h.vocab, zl, labels, logp, lse);
   } else
-    hipLaunchKernelGGL(head_rows_kernel, dim3(h.b), dim3(1024), 0, s, (const float*)(base + w.Z), h.ldz, h.vocab, desc->logit_scale, labels,
-                       logp, lse);
+    hipLaunchKernelGGL(head_rows_kernel, dim3(h.b < kRowGroups ? h.b : kRowGroups), dim3(1024), 0, s, (const float*)(base + w.Z), h.ldz, h.b, h.vocab,
+                       desc->logit_scale, labels, logp, lse);
   HIP_TRY(hipGetLastError());
   return MECEFO_OK;
 }

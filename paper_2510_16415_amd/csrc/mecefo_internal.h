@@ -30,6 +30,9 @@ enum Epilogue : int {
 };
 
 constexpr int kMaxProblems = 4;   // of one launch
+// Rows of kernels that take a wave per row, in workgroups of up to 16 waves: a launch of 2^32 threads or more runs without some of
+// them and reports no error.
+constexpr int64_t kMaxWaveRows = ((int64_t)1 << 26) - 64;
 constexpr int kCUs = 256;         // compute units of the chip
 constexpr int kNormBlocks = 256;  // parts of a matrix whose norms are taken first
 
