@@ -13,10 +13,10 @@ def test_more_rows_than_waves(dtype, d):
     h = B.make_head_desc(MOST + 1, d, 1, dtype)
     refused(UNS, text, B.mecefo_head_workspace_bytes, h, False)
     refused(UNS, text, B.mecefo_head_logprob_fwd, h, at(), None, at(), at(), at(), at(), at(), STREAM)
-    f = B.make_desc(MOST + 1, d, 8, dtype)
+    f = B.make_desc(MOST + 1, d, d, dtype)
     refused(UNS, text, B.mecefo_block_bwd_skip_ex, f, at(), at(), at(), at(), at(), at(), None, None, None, B.SIDE_INPUT, at(512), None, at(), at(),
             at(), 0, at(), stream=STREAM)
-    a = B.make_attn_desc(1, MOST + 1, 1, d)
+    f, a = B.make_desc(1 << 26, d, d, dtype), B.make_attn_desc(8192, 8192, 1, d)
     refused(UNS, text, B.mecefo_block_fwd, f, a, {}, {}, at(), STREAM)
     refused(UNS, text, B.mecefo_block_bwd_full, f, a, {}, {}, 0, at(), STREAM)
     assert B.mecefo_head_workspace_bytes(B.make_head_desc(MOST, d, 1, dtype), False) > 0
