@@ -218,11 +218,11 @@ mecefo_status_t check_desc(const mecefo_head_desc_t* d, bool backward, Head* h) 
   h->esz = h->bf16 ? 2 : 4;
   if (h->bf16 && d->d_model % 8) return FAIL(MECEFO_ERR_UNSUPPORTED, "bf16 path needs d_model to be a multiple of 8 (got %d)", d->d_model);
   if (h->bf16 && (d->ld_act_d % 8 || d->ld_w % 8)) return FAIL(MECEFO_ERR_INVALID_ARG, "bf16 path needs every row stride to be a multiple of 8 elements");
-  if (d->tokens > kMaxWaveRows) return FAIL(MECEFO_ERR_UNSUPPORTED, "more than 2^26 - 64 tokens; split the token batch");
   const bool parts = h->bf16 && !backward;
   if (reaches_2gib(d->tokens, d->ld_act_d, h->esz) || reaches_2gib(d->vocab, d->ld_w, h->esz) ||
       reaches_2gib(d->tokens, parts ? ((int64_t)d->vocab + 31) / 32 : up(d->vocab, 8), parts ? 8 : h->esz))
     return FAIL(MECEFO_ERR_UNSUPPORTED, "a tensor reaches 2 GiB; split the token batch");
+  if (d->tokens > kMaxWaveRows) return FAIL(MECEFO_ERR_UNSUPPORTED, "more than 2^26 - 64 tokens; split the token batch");
   h->b = (int)d->tokens;
   h->dm = d->d_model;
   h->vocab = d->vocab;
