@@ -362,6 +362,10 @@ template <bool PRECISE> __device__ inline SwigluGrad swiglu_grad(float g, float 
 
 template <int EPI> constexpr bool kUnhandledEpilogue = false;
 
+// A sum of exponentials relative to the largest logit as fp32 rounds it, the logits themselves unrounded (one fused multiply-add
+// each): beyond 2^30 that rounding is 2^6 and more, and such sums would leave fp32.  1 then, the largest logit is all that counts; a NaN stays one.
+__device__ inline float held_sum(float s) { return s > 0x1p64f || s < 0x1p-64f ? 1.f : s; }
+
 // EPI_HEAD_GRAD: what a row's gradients are made of; c = 0 where the row has no label among the columns.
 struct HeadRow { float c, lse; int label; };
 __device__ inline HeadRow head_row(const GemmProblem& p, int row) {
@@ -430,7 +434,8 @@ __device__ inline void epilogue_elem(const GemmProblem& p, const KHead& a, int s
     const HeadRow h = head_row(p, row);
     float g = 0.f;
     if (col < p.N && h.c != 0.f) {
-      const float x = v * p.scale - h.lse;
+      float x = v * p.scale - h.lse;
+      x = x > 0.f ? 0.f : x;      // no probability is above 1, however large the logits that fp32 rounds
       g = h.c * ((h.label == col ? 1.f : 0.f) - (PRECISE ? expf(x) : __builtin_amdgcn_exp2f(1.44269504088896341f * x)));
     }
     ((T*)p.C[0])[(int64_t)row * p.ldc + col] = from_f32<T>(g);
@@ -554,7 +559,13 @@ __device__ inline void epilogue_vec8(const GemmProblem& p, const KHead& a, int s
     const float k = p.scale * kLog2e, l = h.lse * kLog2e;
     float o[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = -h.c * __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], k, -l));
+    for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(v[e], k, -l);
+    if (fabsf(l) > 0x1p20f) {     // logits whose rounding matters: no probability is above 1
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = o[e] > 0.f ? 0.f : o[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = -h.c * __builtin_amdgcn_exp2f(o[e]);
     const int at = h.label - col0;
     if (at >= 0 && at < 8) {      // few rows have their label here
 #pragma unroll

@@ -8,12 +8,19 @@
 
 #include "../../include/mecefo.h"
 #include "gemm_bf16_launch.hip.h"
+#include "gemm_common.hip.h"
 #include "mecefo_internal.h"
 
 namespace mecefo {
 namespace {
 
 __device__ inline bool counted(int64_t label, int vocab) { return label >= 0 && label < vocab; }
+
+// A logit is rounded once: fused into z - m it would not be the one that m was taken from.
+__device__ inline float logit(float z, float scale) {
+#pragma clang fp contract(off)
+  return z * scale;
+}
 
 // lse and logp of the rows of fp32 products z (before logit_scale), a workgroup per row, in one pass with a running maximum.
 constexpr int kRowGroups = 1 << 21;      // at most: a launch of 2^32 threads leaves some of them out, without an error
@@ -34,7 +41,7 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(const float* __restrict
       float y[4], m = a.x;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        y[e] = v0 + e < vocab ? x[e] * scale : -INFINITY;
+        y[e] = v0 + e < vocab ? logit(x[e], scale) : -INFINITY;
         m = fmaxf(m, y[e]);
       }
       float s = a.x == -INFINITY ? 0.f : a.y * expf(a.x - m);
@@ -50,7 +57,7 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(const float* __restrict
       for (int w = 1; w < 16; ++w) a = join(a, red[w]);
       const float l = a.x + logf(a.y);
       const int64_t label = labels[row];
-      logp[row] = counted(label, vocab) ? z[label] * scale - l : 0.f;
+      logp[row] = counted(label, vocab) ? logit(z[label], scale) - l : 0.f;
       if (lse) lse[row] = l;
     }
     if (row + gridDim.x < rows) __syncthreads();      // `red` is read
@@ -83,7 +90,7 @@ __global__ __launch_bounds__(1024) void head_parts_kernel(const float2* __restri
   if (threadIdx.x >= ROWS || row >= rows) return;
 #pragma unroll
   for (int w = 1; w < 16; ++w) a = join(a, red[w][r]);
-  const float l = a.x * kLn2 + logf(a.y);
+  const float l = a.x * kLn2 + logf(held_sum(a.y));
   logp[row] = counted(labels[row], vocab) ? zl[row] - l : 0.f;
   if (lse) lse[row] = l;
 }
