@@ -1118,9 +1118,10 @@ mecefo_status_t mecefo_block_full_workspace_bytes(const mecefo_ffn_desc_t* desc,
   return MECEFO_OK;
 }
 
-mecefo_status_t mecefo_block_bwd_full(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn,
+// The standard-mode backward behind mecefo_block_bwd_full.  check_only: nothing is enqueued.
+static mecefo_status_t block_bwd_full(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn,
                                       const mecefo_block_inputs_t* in, const mecefo_block_grads_t* out,
-                                      int accumulate, void* ws, size_t ws_bytes, void* hip_stream) {
+                                      int accumulate, void* ws, size_t ws_bytes, void* hip_stream, bool check_only = false) {
   Ctx c;
   TRY(check_desc(desc, &c));
   TRY(check_attn(c, attn));
@@ -1148,6 +1149,7 @@ mecefo_status_t mecefo_block_bwd_full(const mecefo_ffn_desc_t* desc, const mecef
   }
   if (w.total > ws_bytes) return fail(MECEFO_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, w.total);
   if (!ws) return fail(MECEFO_ERR_INVALID_ARG, "workspace is NULL");
+  if (check_only) return MECEFO_OK;
   Bufs bf;
   bf.base = (char*)up((int64_t)(uintptr_t)ws, 256);
   bf.w = fw;
@@ -1323,6 +1325,12 @@ mecefo_status_t mecefo_block_bwd_full(const mecefo_ffn_desc_t* desc, const mecef
   later = SideJob{};
   TRY(norm_backward(c, attn_norm(), out->dg_attn, accumulate, s, dx_last ? nullptr : &later));
   return dx_last ? MECEFO_OK : wgrads(later);
+}
+
+mecefo_status_t mecefo_block_bwd_full(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn,
+                                      const mecefo_block_inputs_t* in, const mecefo_block_grads_t* out,
+                                      int accumulate, void* ws, size_t ws_bytes, void* hip_stream) {
+  return block_bwd_full(desc, attn, in, out, accumulate, ws, ws_bytes, hip_stream);
 }
 
 mecefo_status_t mecefo_block_fwd_workspace_bytes(const mecefo_ffn_desc_t* desc, const mecefo_attn_desc_t* attn,
@@ -1675,41 +1683,52 @@ mecefo_status_t mecefo_stack_bwd_mixed(const mecefo_ffn_desc_t* desc, const mece
     return fail(MECEFO_ERR_INVALID_ARG, "refresh policy: tau >= 1, power_iters >= 1, cond_steps >= 0, polish_steps >= 0 required");
   const bool left = side == MECEFO_SIDE_OUTPUT;
   // the gradient travels down in dX_bottom's buffer: every layer overwrites its dOut with its dX
-  const void* g = dOut_top;
-  for (int l = n_layers - 1; l >= 0; --l) {
-    const mecefo_block_inputs_t& x = in[l];
-    const mecefo_block_grads_t& o = grads[l];
-    mecefo_status_t st;
-    if (modes[l] == MECEFO_MODE_STANDARD) {           // Alg. 3, first branch: exact gradients, MHA included
-      mecefo_block_inputs_t xi = x;
-      xi.dOut = g;
-      mecefo_block_grads_t oi = o;
-      oi.dX = dX_bottom;
-      st = mecefo_block_bwd_full(desc, attn, &xi, &oi, accumulate, ws, ws_bytes, hip_stream);
-    } else {                                          // neighbor branch
-      const mecefo_layer_lowrank_t& q = lowrank[l];
-      if (policy && mecefo_refresh_due(t[l], policy->tau)) {
-        // V1 of the current weights (Alg. 3: every tau neighbor steps of this layer), warm-started from and
-        // written over the layer's present projection
-        const void* W[3] = {x.Wg, x.Wu, x.Wd};
-        const mecefo_proj_t P[3] = {q.Pg, q.Pu, q.Pd};
-        for (int i = 0; i < 3; ++i) {
-          const int m = i < 2 ? desc->d_ff : desc->d_model, n = i < 2 ? desc->d_model : desc->d_ff;
-          const int64_t ldw = i < 2 ? desc->ld_w_fd : desc->ld_w_df;
-          st = mecefo_projection_refresh(desc->dtype, W[i], m, n, ldw, left ? 1 : 0, P[i].P, P[i].ld, P[i].r,
-                                         policy->power_iters, policy->cond_steps, policy->polish_steps,
-                                         const_cast<void*>(P[i].P), P[i].ld, ws, ws_bytes, hip_stream);
-          if (st != MECEFO_OK) return st;
+  auto pass = [&](bool check_only) -> mecefo_status_t {
+    const void* g = dOut_top;
+    for (int l = n_layers - 1; l >= 0; --l) {
+      const mecefo_block_inputs_t& x = in[l];
+      const mecefo_block_grads_t& o = grads[l];
+      if (modes[l] == MECEFO_MODE_STANDARD) {           // Alg. 3, first branch: exact gradients, MHA included
+        mecefo_block_inputs_t xi = x;
+        xi.dOut = g;
+        mecefo_block_grads_t oi = o;
+        oi.dX = dX_bottom;
+        TRY(block_bwd_full(desc, attn, &xi, &oi, accumulate, ws, ws_bytes, hip_stream, check_only));
+      } else {                                          // neighbor branch
+        const mecefo_layer_lowrank_t& q = lowrank[l];
+        auto backward = [&]() {
+          return block_bwd_skip(desc, x.H, nullptr, g, x.g_ffn, x.Wg, x.Wu, x.Wd, q.Pg, q.Pu, q.Pd, side, nullptr, dX_bottom,
+                                q.dg_ffn, q.dWg, q.dWu, q.dWd, accumulate, ws, ws_bytes, hip_stream, check_only);
+        };
+        if (check_only) TRY(backward());                // and with it the weights and projections that a refresh reads
+        if (policy && mecefo_refresh_due(t[l], policy->tau)) {
+          // V1 of the current weights (Alg. 3: every tau neighbor steps of this layer), warm-started from and
+          // written over the layer's present projection
+          const void* W[3] = {x.Wg, x.Wu, x.Wd};
+          const mecefo_proj_t P[3] = {q.Pg, q.Pu, q.Pd};
+          for (int i = 0; i < 3; ++i) {
+            const int m = i < 2 ? desc->d_ff : desc->d_model, n = i < 2 ? desc->d_model : desc->d_ff;
+            const int64_t ldw = i < 2 ? desc->ld_w_fd : desc->ld_w_df;
+            size_t need = 0;
+            TRY(mecefo_projection_workspace_bytes(desc->dtype, m, n, P[i].r, left ? 1 : 0, &need));
+            if (need > ws_bytes) return fail(MECEFO_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, need);
+            if (check_only) continue;
+            TRY(mecefo_projection_refresh(desc->dtype, W[i], m, n, ldw, left ? 1 : 0, P[i].P, P[i].ld, P[i].r,
+                                          policy->power_iters, policy->cond_steps, policy->polish_steps,
+                                          const_cast<void*>(P[i].P), P[i].ld, ws, ws_bytes, hip_stream));
+          }
+        }
+        if (!check_only) {
+          TRY(backward());
+          if (t) t[l] += 1;                             // Alg. 3: the local step counter of this layer
         }
       }
-      st = mecefo_block_bwd_skip(desc, x.H, g, x.g_ffn, x.Wg, x.Wu, x.Wd, q.Pg, q.Pu, q.Pd, side, dX_bottom,
-                                 q.dg_ffn, q.dWg, q.dWu, q.dWd, accumulate, ws, ws_bytes, hip_stream);
-      if (st == MECEFO_OK && t) t[l] += 1;            // Alg. 3: the local step counter of this layer
+      g = dX_bottom;
     }
-    if (st != MECEFO_OK) return st;
-    g = dX_bottom;
-  }
-  return MECEFO_OK;
+    return MECEFO_OK;
+  };
+  TRY(pass(true));
+  return pass(false);
 }
 
 }  // extern "C"

@@ -1,4 +1,6 @@
 """A stack call that one of its layers makes impossible enqueues nothing: the layers are checked before the first one runs."""
+import ctypes
+
 import pytest
 
 from paper_2510_16415_amd import binding as B
@@ -74,3 +76,36 @@ def test_a_layer_whose_rank_needs_more_workspace():
     refused(WS, "needed", B.mecefo_stack_bwd_skip, DESC, layers(), [at(12288)] * N, q, B.SIDE_INPUT, at(256), at(512), 0, ws(need), STREAM)
     need = B.mecefo_block_ckpt_workspace_bytes(DESC, 8, 8, 8)
     refused(WS, "needed", B.mecefo_stack_bwd_skip_ckpt, DESC, layers(), ckpts(), q, B.SIDE_INPUT, at(256), at(512), 0, ws(need), STREAM)
+
+
+def mixed(modes, bad, change_in=None, change_out=None, q=None, policy=None, counters=None, need=None):
+    inputs, grads = [], []
+    for l in range(N):
+        x = {k: at(2048 + 64 * i) for i, k in enumerate(("X", "H", "g_attn", "g_ffn", "Wq", "Wk", "Wv", "Wo", "Wg", "Wu", "Wd", "Q", "K", "V", "O", "L"))}
+        g = {k: at(12288) for k in ("dg_attn", "dg_ffn", "dWq", "dWk", "dWv", "dWo", "dWg", "dWu", "dWd")}
+        if l == bad:
+            x.update(change_in or {})
+            g.update(change_out or {})
+        inputs.append(x)
+        grads.append(g)
+    need = need or B.mecefo_stack_mixed_workspace_bytes(DESC, ATTN, 8, 8, 8)
+    return (DESC, ATTN, modes, inputs, grads, q or lowrank(), B.SIDE_INPUT, policy, counters, at(256), at(512), 0, ws(need), STREAM)
+
+
+S, NB = B.MODE_STANDARD, B.MODE_NEIGHBOR
+
+
+@pytest.mark.parametrize("modes,args,text", [
+    ([S, S, NB], dict(bad=0, change_in=dict(Wo=None)), "Wo is NULL"), ([S, NB, S], dict(bad=0, change_out=dict(dWk=None)), "every gradient"),
+    ([NB, S, S], dict(bad=0, change_in=dict(H=None)), "H is NULL"), ([NB, NB, S], dict(bad=1, q=lowrank(1, Pd=B.Proj(1 << 20, 65, 72))), "rank 65")])
+def test_mixed_backward(modes, args, text):
+    refused(INV, text, B.mecefo_stack_bwd_mixed, *mixed(modes, **args))
+
+
+def test_mixed_backward_whose_refresh_needs_more_workspace():
+    need = max(B.mecefo_block_full_workspace_bytes(DESC, ATTN), B.mecefo_workspace_bytes(DESC, 8, 8, 8))
+    refresh = max(B.mecefo_projection_workspace_bytes(B.BF16, m, n, r) for m, n, r in ((64, 32, 8), (32, 64, 8)))
+    assert need < refresh
+    counters = (ctypes.c_int64 * N)(*[0] * N)
+    refused(WS, "needed", B.mecefo_stack_bwd_mixed, *mixed([NB, NB, S], None, policy=B.RefreshPolicy(5, 1, 0, 1), counters=counters, need=need))
+    assert list(counters) == [0] * N
