@@ -362,8 +362,9 @@ mecefo_status_t mecefo_block_bwd_skip_ex(const mecefo_ffn_desc_t* desc, const vo
 /* ---- 8-bit activation checkpoints (Sec. 3.3 keeps one tensor per layer; here in half the bytes of bf16).
  * A row is cut into groups of 32 columns; a group holds 32 signed bytes q and one byte e and stands for the values
  * q * 2^(e - 127).  Packing: e - 127 is the exponent of the group's largest magnitude less 6 (not below -126), q is
- * x * 2^(127 - e) rounded to the nearest whole number, halves to even, at most 127.  So |x - q 2^(e-127)| is at most
- * half a step 2^(e-127), 1/128 of the group's largest magnitude, for every x of a bf16 tensor (for fp32 up to a whole step where x is beyond 127.5 steps).
+ * x * 2^(127 - e) rounded to the nearest whole number, halves to even, at most 127.  So |x - q 2^(e-127)| is at most half a
+ * step 2^(e-127) for every x of a bf16 tensor (for fp32 up to a whole step where x is beyond 127.5 steps); half a step is 1/128
+ * of the group's largest magnitude or less where that is at least 2^-120, and 2^-127 below.
  * A group that holds an infinity or a NaN is stored as e = 255 and q = 0 and stands for NaN in all its columns.
  * Every value that a checkpoint stands for is a bf16 number: unpacking is exact in either dtype.
  * q [rows x ld_q]: 16-byte aligned, ld_q a multiple of 16 and >= 32 ceil(cols / 32); the columns behind cols are written as
@@ -413,8 +414,9 @@ mecefo_status_t mecefo_stack_bwd_skip_ckpt(const mecefo_ffn_desc_t* desc, int n_
  * part in the gradient, nor has one whose dlogp is 0 (its row of X has to be finite all the same).  Large bf16 backwards leave such
  * rows out of their products; which rows these are is read on the device, so a captured graph follows the labels and dlogp of
  * each replay.
- * The logits are never stored by the forward.  dtype MECEFO_BF16: products accumulated in fp32, exponentials and their
- * sums in fp32; with gamma, U is rounded to bf16.  d_model must be a multiple of 8, vocab may be any size.
+ * dtype MECEFO_BF16: the forward stores no logits (MECEFO_F32: in the workspace); products accumulated in fp32, exponentials and
+ * their sums in fp32; dz, and with gamma U and dU, are rounded to bf16, whatever grad_dtype is.  d_model must be a multiple of 8,
+ * vocab may be any size.
  * The backward forms the products again and stores dz_iv = logit_scale * dlogp_i * ([v = labels[i]] - exp(z_iv - lse_i)) in
  * dtype (b * up8(vocab) elements of the workspace, which must stay below 2 GiB, as must X and W: split the token batch and
  * accumulate; so must the products that the fp32 forward stores, and the bf16 forward's b * ceil(vocab / 32) parts of 8 bytes);

@@ -743,7 +743,8 @@ mecefo_status_t check_clear(const Ctx& c, const Ckpt& k, int cols, const char* n
   return MECEFO_OK;
 }
 
-// The neighbor-mode backward behind its entry points.  kept: the stored tensors as 8-bit checkpoints, which are unpacked
+// The neighbor-mode backward behind its entry points.  bf16: U, dA, dG, dZ, A and dU are rounded to bf16, as operands of the products
+// and of the norm's backward; the weight gradients are off by 3.3e-3 to 4.5e-3 (norm) where one rounding of the exact ones is 1.7e-3.  kept: the stored tensors as 8-bit checkpoints, which are unpacked
 // into the workspace (H, opt->G and opt->Z are then NULL), or NULL.  check_only: nothing is enqueued.
 mecefo_status_t block_bwd_skip(const mecefo_ffn_desc_t* desc, const void* H, const KeptCkpts* kept, const void* dOut,
                                const void* gamma, const void* Wg, const void* Wu, const void* Wd,

@@ -3,6 +3,9 @@
 //   U = norm(X) gamma (or X),  z = logit_scale U W^T [b x V],  lse_i = log sum_v exp z_iv,  logp_i = z_i,label - lse_i
 //   dz_iv = logit_scale dlogp_i (1[v = label_i] - exp(z_iv - lse_i)),  dU = dz W,  dW = dz^T U
 // Everything that is large is a product on the GEMM core: 2 b d V operations forward, 6 b d V backward (z is formed again).
+// bf16 roundings: dz, because dU and dW are bf16 products of it (two bf16 halves of dz would double them), 2.2e-3 on either against
+// 1.7e-3 for the result's own rounding; with a gain U, an operand as well, and dU, which the norm's backward reads as the blocks' norms
+// read theirs (in fp32 its bytes would double).  Of few tokens dU is added up from fp32 parts and rounded once.
 #include <math.h>
 #include <string.h>
 

@@ -3,8 +3,8 @@
 // each begins, and a mask which tokens count.  A few bytes per token: the launches and the latency of the loads are what they
 // take, so every sequence is cut into slices, a workgroup each, in two launches: one takes the sums that the gradient of a
 // token depends on (its sequence's ratio, the number of counted tokens), the other the tokens' gradients.  A small batch is one
-// workgroup's, and one launch's.  Sums are held in 64
-// bits, each added up in an order that only the sizes decide.
+// workgroup's, and one launch's; a policy batch of many sequences has a launch in between.  Sums are held in 64 bits, each added up
+// in an order that only the sizes decide; exponentials of the policy in 32 bits where they hold them, else in 64.
 #include <math.h>
 
 #include <type_traits>
