@@ -427,7 +427,7 @@ typedef struct {
   int64_t ld_act_d, ld_w;       /* row strides of X and dX [b x d], of W and dW [V x d] */
   mecefo_dtype_t dtype;         /* X, gamma, W, dX */
   mecefo_dtype_t grad_dtype;    /* dW, dgamma: MECEFO_F32, or equal to dtype */
-  float logit_scale;            /* 1 / temperature; any finite number that leaves the logits finite.  fp32 holds a logit to 2^-24 of
+  float logit_scale;            /* 1 / temperature; at most 2^127 either way, and so the logits.  fp32 holds a logit to 2^-24 of
                                    itself: from about 1e5 on that is seen in logp and in the gradient's exp(z - lse) (at most 1) */
   float rms_eps;                /* used only with gamma */
 } mecefo_head_desc_t;

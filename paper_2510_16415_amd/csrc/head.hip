@@ -222,7 +222,8 @@ mecefo_status_t check_desc(const mecefo_head_desc_t* d, bool backward, Head* h) 
   if (d->grad_dtype != MECEFO_F32 && d->grad_dtype != d->dtype) return FAIL(MECEFO_ERR_UNSUPPORTED, "grad_dtype must be MECEFO_F32 or equal to dtype");
   if (d->tokens < 0 || d->d_model < 1 || d->vocab < 1) return FAIL(MECEFO_ERR_INVALID_ARG, "tokens >= 0, d_model >= 1, vocab >= 1 required");
   if (d->ld_act_d < d->d_model || d->ld_w < d->d_model) return FAIL(MECEFO_ERR_INVALID_ARG, "a row stride is smaller than the logical width");
-  if (!isfinite(d->logit_scale)) return FAIL(MECEFO_ERR_INVALID_ARG, "logit_scale must be finite");
+  // times log2(e) it is still a number
+  if (!(fabsf(d->logit_scale) <= 0x1p127f)) return FAIL(MECEFO_ERR_INVALID_ARG, "logit_scale must be a number of at most 2^127");
   h->d = d;
   h->bf16 = d->dtype == MECEFO_BF16;
   h->esz = h->bf16 ? 2 : 4;
