@@ -290,10 +290,10 @@ __device__ inline void head_lse_rows(const GemmProblem& p, const f32x4_t (&acc)[
           s += !EDGE || 16 * j + c0 < left ? x : 0.f;
         }
         s = row16(s, [](float x, float y) { return x + y; });
-        if (c0 == 4 * (i - i0) + e) mine = float2{top, held_sum(s)};
+        if (c0 == 4 * (i - i0) + e) mine = float2{top, s};
       }
     const int row = row_w + 16 * (i0 + (c0 >> 2)) + 4 * (lane >> 4) + (c0 & 3);
-    if (i0 + (c0 >> 2) < TM && row < p.M) out[row] = mine;
+    if (i0 + (c0 >> 2) < TM && row < p.M) out[row] = float2{mine.x, held_sum(mine.y)};
   }
 }
 
