@@ -475,7 +475,7 @@ mecefo_status_t mecefo_preference_loss(const mecefo_preference_desc_t* desc, con
  * loss = sum of w l with w = 1 / counted tokens (MECEFO_MEAN_TOKENS), or 1 / (counted tokens of the sequence * sequences that
  * have any) (MECEFO_MEAN_SEQUENCES); 0 where nothing is counted.  kl and clipped: the same means of KL and of whether the bound
  * is what min() takes; loss, kl and clipped are [1], the last two may be NULL.  A token on a bound still has its gradient.
- * advantage: [tokens] (advantage_per_token) or [sequences].  ref_logp may be NULL where kl_coef is 0. */
+ * advantage: [tokens] (advantage_per_token) or [sequences].  ref_logp may be NULL where kl_coef is 0, or without tokens. */
 typedef enum { MECEFO_MEAN_TOKENS = 0, MECEFO_MEAN_SEQUENCES = 1 } mecefo_loss_mean_t;
 typedef struct {
   int64_t tokens;

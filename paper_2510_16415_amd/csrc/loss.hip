@@ -658,7 +658,7 @@ mecefo_status_t mecefo_policy_loss(const mecefo_policy_desc_t* desc, const float
   TRY(check_align(advantage, "advantage", 4, any && desc->sequences > 0)); TRY(check_align(offsets, "offsets", 8, desc->sequences > 0));
   TRY(check_align(loss, "loss", 4, true)); TRY(check_align(kl, "kl", 4, false)); TRY(check_align(clipped, "clipped", 4, false));
   TRY(check_align(dlogp, "dlogp", 4, any));
-  if (!ref_logp && desc->kl_coef != 0.f) return (mecefo_status_t)fail(MECEFO_ERR_INVALID_ARG, "kl_coef needs ref_logp");
+  if (any && !ref_logp && desc->kl_coef != 0.f) return (mecefo_status_t)fail(MECEFO_ERR_INVALID_ARG, "kl_coef needs ref_logp");
   TRY(check_ws(policy_bytes(desc), ws, ws_bytes));
   const size_t tokens = (size_t)desc->tokens, seqs = (size_t)desc->sequences;
   const Span spans[] = {{loss, 4, "loss", true}, {kl, 4, "kl", true}, {clipped, 4, "clipped", true}, {dlogp, 4 * tokens, "dlogp", true},

@@ -117,3 +117,12 @@ def test_a_gradient_that_its_weight_brings_back_into_fp32(seqs, mean_len, by_seq
             assert abs(got["loss"][0] - want["loss"]) <= TOL * max(size, abs(want["loss"]))
         if want["kl"] < 3e38:
             assert abs(got["kl"][0] - want["kl"]) <= 101 * TOL * want["kl"]
+
+
+@pytest.mark.parametrize("seqs", [0, 3, 40, 3000])
+@pytest.mark.parametrize("by_seq", [False, True])
+def test_a_batch_without_tokens_and_a_kl_term(seqs, by_seq):
+    """Empty arrays have no address, the reference's among them."""
+    none = np.zeros(0, np.float32)
+    got = run_policy(none, none, none, np.ones(seqs, np.float32), None, np.zeros(seqs + 1, np.int64), kl=0.05, by_seq=by_seq)
+    assert got["loss"][0] == 0 and got["kl"][0] == 0 and got["clipped"][0] == 0
